@@ -2,7 +2,8 @@
 
 The binding marshals arguments only; every step of the path runs in the HIP
 kernels behind the C ABI (include/hps.h); the host-memory cache behind the table
-(include/hps_mem.h) is native host code.  torch supplies device memory and the
+(include/hps_mem.h) is native host code.  mx4.py: the operators on frozen rows
+(include/hps_mx4.h).  torch supplies device memory and the
 current stream.
 """
 from .binding import (  # noqa: F401
@@ -21,5 +22,15 @@ from .binding import (  # noqa: F401
     ROWS_F32_WIDE,
     OK, EINVAL, EFULL, ERESERVED, ESTATE, EDEVICE, ENOMEM,
     EXPORTS,
+    EXPORTS_MX4,
     STAGES,
+)
+from .mx4 import (  # noqa: F401
+    LogProbs,
+    Mx4Rows,
+    mx4_logprobs,
+    mx4_logprobs_backward,
+    mx4_quantize,
+    mx4_scores,
+    MX4_MAX_TOP,
 )

@@ -19,6 +19,11 @@ EXPORTS = ("hps_table_bytes", "hps_workspace_bytes", "hps_create", "hps_insert",
            "hps_mem_create", "hps_mem_fetch", "hps_mem_store", "hps_mem_complete_batch",
            "hps_mem_take_evicted", "hps_mem_list", "hps_mem_stats", "hps_mem_destroy")
 
+# include/hps_mx4.h
+EXPORTS_MX4 = ("hps_mx4_row_bytes", "hps_mx4_row_scales", "hps_mx4_quantize", "hps_mx4_dequantize", "hps_mx4_get",
+               "hps_mx4_scores", "hps_mx4_logprobs_bytes", "hps_mx4_logprobs", "hps_mx4_logprobs_backward_bytes",
+               "hps_mx4_logprobs_backward")
+
 STAGES = ("sort", "unique", "lookup", "pool", "push")
 
 
@@ -41,6 +46,11 @@ class MemStats(ctypes.Structure):
     _fields_ = [("lru_size", ctypes.c_uint64), ("lfu_size", ctypes.c_uint64),
                 ("pinned", ctypes.c_uint64), ("evicted_waiting", ctypes.c_uint64),
                 ("hits", ctypes.c_uint64), ("misses", ctypes.c_uint64)]
+
+
+class Mx4Operand(ctypes.Structure):
+    """hps_mx4_rows."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n", ctypes.c_uint64)]
 
 
 _lib = None
@@ -118,6 +128,27 @@ def lib() -> ctypes.CDLL:
         L.hps_mem_stats.argtypes = [vp, ctypes.POINTER(MemStats)]
         L.hps_mem_destroy.restype = st
         L.hps_mem_destroy.argtypes = [vp]
+        f32, i32, rows = ctypes.c_float, ctypes.c_int, ctypes.POINTER(Mx4Operand)
+        L.hps_mx4_row_bytes.restype = sz
+        L.hps_mx4_row_bytes.argtypes = [u32]
+        L.hps_mx4_row_scales.restype = sz
+        L.hps_mx4_row_scales.argtypes = [u32]
+        L.hps_mx4_quantize.restype = st
+        L.hps_mx4_quantize.argtypes = [vp, i32, u64, u32, u64, vp, vp, vp, vp]
+        L.hps_mx4_dequantize.restype = st
+        L.hps_mx4_dequantize.argtypes = [rows, u32, vp, vp]
+        L.hps_mx4_get.restype = st
+        L.hps_mx4_get.argtypes = [vp, vp, u64, vp, vp, vp, vp]
+        L.hps_mx4_scores.restype = st
+        L.hps_mx4_scores.argtypes = [rows, rows, u32, f32, vp, vp, i32, u64, vp]
+        L.hps_mx4_logprobs_bytes.restype = sz
+        L.hps_mx4_logprobs_bytes.argtypes = [u64, u64, u32, u32]
+        L.hps_mx4_logprobs.restype = st
+        L.hps_mx4_logprobs.argtypes = [rows, rows, u32, f32, vp, vp, u32, u32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.hps_mx4_logprobs_backward_bytes.restype = sz
+        L.hps_mx4_logprobs_backward_bytes.argtypes = [u64, u64, u32]
+        L.hps_mx4_logprobs_backward.restype = st
+        L.hps_mx4_logprobs_backward.argtypes = [rows, rows, u32, f32, vp, vp, vp, vp, vp, u32, vp, vp, vp, sz, vp]
         L.hps_strerror.restype = ctypes.c_char_p
         L.hps_strerror.argtypes = [st]
         _lib = L
@@ -257,6 +288,17 @@ class HpsTable:
         _check(lib().hps_get_or_zero(self._h, _ptr(keys), n, _ptr(w), _ptr(a), _ptr(f), _stream()),
                "hps_get_or_zero")
         return w, a, f
+
+    def get_mx4(self, keys):
+        """get() into the 4-bit form: (Mx4Rows, found).  Rows of absent keys are zeros."""
+        import torch
+        from .mx4 import Mx4Rows
+        n = keys.numel()
+        rows = Mx4Rows.empty(n, self.dim, self.device)
+        f = torch.empty(n, dtype=torch.bool, device=self.device)
+        _check(lib().hps_mx4_get(self._h, _ptr(keys), n, _ptr(rows.codes), _ptr(rows.scales), _ptr(f), _stream()),
+               "hps_mx4_get")
+        return rows, f
 
     def set_pooling(self, mean: bool) -> None:
         """Bags are summed (False, the default) or averaged (True) from the next pull on."""

@@ -5,6 +5,7 @@
 #include "../../include/hps.h"
 #include "../../include/hps_measure.h"
 #include "../../include/hps_mem.h"
+#include "../../include/hps_mx4.h"
 
 #include <hip/hip_runtime.h>
 
@@ -13,6 +14,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include <algorithm>
@@ -29,6 +31,10 @@
 #include "sort.hpp"
 #include "table.hpp"
 #include "mem_tier.hpp"
+#include "mx4.hpp"
+#include "mx4_backward.hpp"
+#include "mx4_logprobs.hpp"
+#include "mx4_scores.hpp"
 
 using namespace hps;
 
@@ -1584,3 +1590,5 @@ hps_status hps_mem_destroy(hps_mem* m) {
 }
 
 }  // extern "C"
+
+#include "mx4_host.hpp"

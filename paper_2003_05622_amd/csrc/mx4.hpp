@@ -1,0 +1,232 @@
+// Rows in microscaled 4-bit floating point (include/hps_mx4.h): the form itself, and the kernels that bring
+// rows into it (from an array, from the table by key) and read them back.
+//
+// A block of 32 values x has the scale 2^E, E = floor(log2 max|x|) - 2, so that the largest magnitude
+// lies in [4, 8) scales; a value becomes the code nearest to x / 2^E.  E comes from the exponent bits
+// of the largest magnitude, compared as whole numbers (a NaN is then the largest of all); the code from the
+// GPU's conversion instruction, which divides by the scale exactly, rounds to nearest even and saturates.
+#pragma once
+
+#include "common.hpp"
+#include "rows.hpp"
+#include "table.hpp"
+
+namespace hps {
+
+constexpr u32 kMxBlock = 32;          // values that share a scale
+constexpr u32 kMxNoScale = 255;       // the scale byte of a block that stands for NaN
+
+// Bytes of codes a row takes: whole blocks, so that a block is one aligned 16-byte word; rows of a quarter or
+// half a block only that (narrow rows are many).
+__host__ __device__ constexpr u32 mx_row_bytes(u32 dim) { return dim <= 8 ? 4u : dim <= 16 ? 8u : (dim + kMxBlock - 1) / kMxBlock * 16; }
+__host__ __device__ constexpr u32 mx_blocks(u32 dim) { return (dim + kMxBlock - 1) / kMxBlock; }
+
+// Eight values of a block's lane group: the group of GL lanes (4; narrow rows: 1 or 2) holds a whole block.
+struct MxEight {
+  float v[8];
+  __device__ __forceinline__ void set(int q, float4 f) { v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w; }
+};
+
+// The scale byte of the block whose values the lane group holds, and the lane's eight codes.
+template <int GL>
+__device__ __forceinline__ u32 mx_encode(const MxEight& x, u32* codes) {
+  u32 most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x.v[i]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int d = 1; d < GL; d *= 2) most = max(most, (u32)__shfl_xor((int)most, d, kWave));
+  const u32 e = most >> 23;
+  if (e == 255) {
+    *codes = 0;
+    return kMxNoScale;
+  }
+  const u32 scale = e > 2 ? e - 2 : 0;
+  // (2^-127 is below the normal numbers)
+  const float s = __uint_as_float(scale ? scale << 23 : 0x00400000u);
+  u32 c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[0], x.v[1], s, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2], x.v[3], s, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[4], x.v[5], s, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[6], x.v[7], s, 3);
+  *codes = c;
+  return scale;
+}
+
+// What eight codes of a block stand for.
+__device__ __forceinline__ MxEight mx_decode(u32 codes, u32 scale) {
+  const float s = scale == kMxNoScale ? __uint_as_float(0x7FC00000u) : __uint_as_float(scale ? scale << 23 : 0x00400000u);
+  MxEight x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const u32 c = codes >> (4 * i) & 15u, m = c & 7u;
+    // two exponent bits (bias 1) and a fraction bit; without exponent bits 0 or a half
+    const float one = m >= 2 ? __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22) : 0.5f * (float)m;
+    x.v[i] = (c & 8u ? -one : one) * s;
+  }
+  return x;
+}
+
+constexpr int kMxThreads = 256;
+
+// Lane groups a block's codes take: a group's lanes hold eight values each.
+__host__ __device__ constexpr int mx_group_lanes(u32 dim) { return dim <= 8 ? 1 : dim <= 16 ? 2 : 4; }
+
+template <bool BF16>
+__device__ __forceinline__ float4 load_values4(const void* base, u64 at) {
+  if (BF16) {
+    const uint2 raw = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at);
+    return make_float4(bf16_value(raw.x & 0xFFFFu), bf16_value(raw.x >> 16), bf16_value(raw.y & 0xFFFFu), bf16_value(raw.y >> 16));
+  }
+  return *reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
+}
+
+// One lane group per block, flat over all blocks.
+template <bool BF16, int GL>
+__global__ void __launch_bounds__(kMxThreads)
+mx_quantize(const void* __restrict__ values, u64 n, u32 dim, u64 stride, uint8_t* __restrict__ codes,
+            uint8_t* __restrict__ scales, float* __restrict__ rounded) {
+  const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
+  const u64 total = n * blocks;
+  for (u64 b = ((u64)blockIdx.x * kMxThreads + threadIdx.x) / GL; b < total; b += (u64)gridDim.x * (kMxThreads / GL)) {
+    const u64 row = b / blocks;
+    const u32 block = (u32)(b - row * blocks), sub = threadIdx.x % GL, col = block * kMxBlock + 8 * sub;
+    MxEight x;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      x.set(q, col + 4 * q < dim ? load_values4<BF16>(values, row * stride + col + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f));
+    u32 c;
+    const u32 scale = mx_encode<GL>(x, &c);
+    *reinterpret_cast<u32*>(codes + row * row_bytes + block * 16 + 4 * sub) = c;
+    if (sub == 0) scales[b] = (uint8_t)scale;
+    if (rounded) {
+      const MxEight y = mx_decode(c, scale);
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        if (col + 4 * q < dim)
+          *reinterpret_cast<float4*>(rounded + row * dim + col + 4 * q) = make_float4(y.v[4 * q], y.v[4 * q + 1], y.v[4 * q + 2], y.v[4 * q + 3]);
+    }
+  }
+}
+
+// Eight values a lane.
+__global__ void __launch_bounds__(kMxThreads)
+mx_dequantize(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, u64 n, u32 dim, float* __restrict__ out) {
+  const u32 words = (dim + 7) / 8, row_bytes = mx_row_bytes(dim), blocks = mx_blocks(dim);
+  const u64 total = n * words;
+  for (u64 i = (u64)blockIdx.x * kMxThreads + threadIdx.x; i < total; i += (u64)gridDim.x * kMxThreads) {
+    const u64 row = i / words;
+    const u32 word = (u32)(i - row * words);
+    const MxEight y = mx_decode(*reinterpret_cast<const u32*>(codes + row * row_bytes + 4 * word), scales[row * blocks + word / 4]);
+    float* to = out + row * dim + 8 * word;
+    *reinterpret_cast<float4*>(to) = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
+    if (8 * word + 4 < dim) *reinterpret_cast<float4*>(to + 4) = make_float4(y.v[4], y.v[5], y.v[6], y.v[7]);
+  }
+}
+
+// Rows of the table by key.  As get_rows: a wave finds 64 keys, one per lane, and then goes through their
+// blocks, a lane group per block.
+template <bool BF16, int GL>
+__global__ void __launch_bounds__(kRowThreads)
+mx_get(TableView t, const u64* __restrict__ keys, u64 n_keys, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+       uint8_t* __restrict__ found_out) {
+  const bool failed = load_error(t.st) != 0;
+  const u32 lane = lane_id(), sub = lane % kLookupLanes;
+  const u32 blocks = mx_blocks(t.dim), row_bytes = mx_row_bytes(t.dim);
+  const u64 n_waves = (u64)gridDim.x * (kRowThreads / kWave);
+  for (u64 first = ((u64)blockIdx.x * (kRowThreads / kWave) + threadIdx.x / kWave) * kWave; first < n_keys;
+       first += n_waves * kWave) {
+    const u64 u = first + lane;
+    u64 key = u < n_keys && !failed ? keys[u] : kEmptyKey, line;
+    u32 row, free_at;
+    search_keys<kLookupLanes>(t, &key, &line, &row, &free_at, sub);
+    if (u < n_keys) found_out[u] = row != kNoRow;
+    else row = kSkipRow;
+    const u32 part = lane % GL;
+    for (u32 i = 0; i < blocks * GL; ++i) {            // 64 keys x blocks, 64 / GL blocks a turn
+      const u32 at = (i * kWave + lane) / GL, k = at / blocks, block = at - k * blocks, col = block * kMxBlock + 8 * part;
+      const u32 r = (u32)__shfl((int)row, (int)k, kWave);
+      MxEight x;
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        x.set(q, r < kSkipRow && col + 4 * q < t.dim ? load_w4_as<BF16>(t, r, col / 4 + q) : make_float4(0.f, 0.f, 0.f, 0.f));
+      u32 c;
+      const u32 scale = mx_encode<GL>(x, &c);
+      if (r == kSkipRow) continue;
+      *reinterpret_cast<u32*>(codes + (first + k) * row_bytes + block * 16 + 4 * part) = c;
+      if (part == 0) scales[(first + k) * blocks + block] = (uint8_t)scale;
+    }
+  }
+}
+
+// ---- products of held rows ---------------------------------------------------------------------
+// v_mfma_scale_f32_32x32x64: D (32 x 32) += A (32 x 64) B (64 x 32), both in 4 bits with a scale per block.  Lane
+// l holds one block (16 bytes) of row l % 32 of either operand, the first or the second of the 64 values by
+// l / 32, and that block's scale byte; of D it holds column l % 32 (B's row) and, as element r, row
+// mx_row_of(r, l / 32) (A's row).
+typedef int MxOperand __attribute__((ext_vector_type(8)));
+typedef float MxTile __attribute__((ext_vector_type(16)));
+constexpr u32 kMxTile = 32;
+
+__device__ __forceinline__ u32 mx_row_of(u32 r, u32 half) { return 8 * (r >> 2) + 4 * half + (r & 3u); }
+
+struct MxHeld {            // rows as a kernel sees them
+  const uint8_t* codes;
+  const uint8_t* scales;
+  u32 n;
+};
+
+// Block `block` of row `row` (below n), of 2^-127 zeros where the row has no such block.  WIDTH: bytes of a
+// block (16, or those of a whole narrow row).
+template <int WIDTH>
+__device__ __forceinline__ void mx_load(const MxHeld& m, u32 row, u32 block, u32 blocks, MxOperand* codes, u32* scale) {
+  MxOperand c = {0, 0, 0, 0, 0, 0, 0, 0};
+  *scale = 0;
+  if (block < blocks) {
+    if (WIDTH == 16) {
+      const int4 w = *reinterpret_cast<const int4*>(m.codes + ((u64)row * blocks + block) * 16);
+      c[0] = w.x; c[1] = w.y; c[2] = w.z; c[3] = w.w;
+    } else if (WIDTH == 8) {
+      const int2 w = *reinterpret_cast<const int2*>(m.codes + (u64)row * 8);
+      c[0] = w.x; c[1] = w.y;
+    } else {
+      c[0] = *reinterpret_cast<const int*>(m.codes + (u64)row * 4);
+    }
+    *scale = m.scales[(u64)row * blocks + block];
+  }
+  *codes = c;
+}
+
+__device__ __forceinline__ MxTile mx_multiply(const MxOperand& a, u32 a_scale, const MxOperand& b, u32 b_scale, MxTile d) {
+  constexpr int kFp4 = 4;
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, kFp4, kFp4, 0, (int)a_scale, 0, (int)b_scale);
+}
+
+// The products of 32 rows of `a` and 32 of `b`; a_row / b_row: the row that lane l % 32 brings.
+template <int WIDTH>
+__device__ __forceinline__ MxTile mx_products(const MxHeld& a, u32 a_row, const MxHeld& b, u32 b_row, u32 blocks) {
+  const u32 half = lane_id() / 32;
+  MxTile d;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) d[r] = 0.f;
+  for (u32 s = 0; s < blocks; s += 2) {
+    MxOperand ca, cb;
+    u32 sa, sb;
+    mx_load<WIDTH>(a, a_row, s + half, blocks, &ca, &sa);
+    mx_load<WIDTH>(b, b_row, s + half, blocks, &cb, &sb);
+    d = mx_multiply(ca, sa, cb, sb, d);
+  }
+  return d;
+}
+
+// A score; a row whose bias is not finite is out, whatever its codes are.
+__device__ __forceinline__ float mx_bias(const float* bias, u32 row) {
+  const float b = bias[row];
+  return (__float_as_uint(b) & 0x7F800000u) == 0x7F800000u ? -__builtin_huge_valf() : b;
+}
+template <bool BIAS>
+__device__ __forceinline__ float mx_score(float dot, float scale, float bias) {
+  if (!BIAS) return __fmul_rn(dot, scale);
+  return bias == -__builtin_huge_valf() ? bias : __fmaf_rn(dot, scale, bias);
+}
+
+}  // namespace hps

@@ -1,0 +1,220 @@
+// Host side of include/hps_mx4.h: argument checks, the division of the work, launches.  Part of hps.hip.
+#pragma once
+
+namespace {
+
+constexpr uint64_t kMxMaxQueries = 1ull << 20;
+constexpr uint64_t kMxMaxRows = (1ull << 31) - 1;
+constexpr uint64_t kMxMaxBlocks = 1ull << 30;      // workgroups a launch may have
+
+bool mx_dim_ok(uint32_t dim) { return dim >= 4 && dim <= 1024 && dim % 4 == 0; }
+bool mx_aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+size_t mx_code_alignment(uint32_t dim) { return std::min<size_t>(16, mx_row_bytes(dim)); }
+
+bool mx_rows_ok(const hps_mx4_rows* r, uint32_t dim, uint64_t most) {
+  if (!r || r->n > most) return false;
+  return r->n == 0 || (r->d_codes && r->d_scales && mx_aligned(r->d_codes, mx_code_alignment(dim)));
+}
+MxHeld mx_held(const hps_mx4_rows* r) { return {r->d_codes, r->d_scales, (u32)r->n}; }
+
+uint64_t mx_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// How the rows are dealt out over the waves: so many parts that the GPU is full.
+constexpr uint64_t kMxWaves = 4096;
+struct MxSplit {
+  uint64_t query_tiles, part_rows, parts, group, groups;
+};
+MxSplit mx_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top, uint64_t waves) {
+  MxSplit s;
+  s.query_tiles = mx_ceil(n_queries, kMxTile);
+  // rows of a group: what noting the groups' highest scores costs (4 bytes a group, written and read) against scoring the rows of
+  // `top` groups once more
+  s.group = kMxTile;
+  const double row = mx_row_bytes(dim) + mx_blocks(dim);
+  while (top && s.group < 1024 && 8.0 * n_rows / (double)s.group > (double)top * (double)(2 * s.group) * row) s.group *= 2;
+  const uint64_t wanted = std::max<uint64_t>(1, waves / s.query_tiles);
+  s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), s.group) * s.group;
+  s.parts = mx_ceil(n_rows, s.part_rows);
+  s.groups = top ? mx_ceil(n_rows, s.group) : 0;
+  return s;
+}
+size_t mx_parts_bytes(const MxSplit& s, uint64_t n_queries) { return align_up(s.parts * n_queries * sizeof(MxPart)); }
+
+template <typename F>
+void mx_by_width(uint32_t dim, F f) {
+  if (dim <= 8) f(std::integral_constant<int, 4>());
+  else if (dim <= 16) f(std::integral_constant<int, 8>());
+  else f(std::integral_constant<int, 16>());
+}
+template <typename F>
+void mx_by_flag(bool flag, F f) {
+  if (flag) f(std::true_type());
+  else f(std::false_type());
+}
+
+bool mx_scale_ok(float scale) { return scale - scale == 0.f; }     // (finite)
+
+}  // namespace
+
+extern "C" {
+
+size_t hps_mx4_row_bytes(uint32_t dim) { return mx_dim_ok(dim) ? mx_row_bytes(dim) : 0; }
+size_t hps_mx4_row_scales(uint32_t dim) { return mx_dim_ok(dim) ? mx_blocks(dim) : 0; }
+
+hps_status hps_mx4_quantize(const void* d_values, hps_value_type type, uint64_t n, uint32_t dim, uint64_t stride,
+                            uint8_t* d_codes, uint8_t* d_scales, float* d_rounded, void* stream) {
+  if (!mx_dim_ok(dim) || (type != HPS_VALUES_F32 && type != HPS_VALUES_BF16) || stride < dim || stride % 4) return HPS_EINVAL;
+  if (n > (1ull << 40) || stride > (1ull << 40) / std::max<uint64_t>(n, 1)) return HPS_EINVAL;
+  if (n == 0) return HPS_OK;
+  if (!d_values || !d_codes || !d_scales) return HPS_EINVAL;
+  if (!mx_aligned(d_values, type == HPS_VALUES_F32 ? 16 : 8) || !mx_aligned(d_codes, mx_code_alignment(dim)) || !mx_aligned(d_rounded, 16))
+    return HPS_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  mx_by_width(dim, [&](auto width) {
+    constexpr int GL = decltype(width)::value / 4;
+    const unsigned blocks = grid_for(n * mx_blocks(dim), kMxThreads / GL, 1u << 20);
+    mx_by_flag(type == HPS_VALUES_BF16, [&](auto bf16) {
+      mx_quantize<decltype(bf16)::value, GL><<<blocks, kMxThreads, 0, s>>>(d_values, n, dim, stride, d_codes, d_scales, d_rounded);
+    });
+  });
+  return launch_ok() ? HPS_OK : HPS_EDEVICE;
+}
+
+hps_status hps_mx4_dequantize(const hps_mx4_rows* rows, uint32_t dim, float* d_out, void* stream) {
+  if (!mx_dim_ok(dim) || !mx_rows_ok(rows, dim, 1ull << 30)) return HPS_EINVAL;
+  if (rows->n == 0) return HPS_OK;
+  if (!d_out || !mx_aligned(d_out, 16)) return HPS_EINVAL;
+  mx_dequantize<<<grid_for(rows->n * mx_ceil(dim, 8), kMxThreads, 1u << 20), kMxThreads, 0, static_cast<hipStream_t>(stream)>>>(
+      rows->d_codes, rows->d_scales, rows->n, dim, d_out);
+  return launch_ok() ? HPS_OK : HPS_EDEVICE;
+}
+
+hps_status hps_mx4_get(hps_table* t, const uint64_t* d_keys, uint64_t n, uint8_t* d_codes, uint8_t* d_scales,
+                       uint8_t* d_found_out, void* stream) {
+  if (!t || (n && (!d_keys || !d_codes || !d_scales || !d_found_out || !mx_aligned(d_codes, mx_code_alignment(t->dim))))) return HPS_EINVAL;
+  if (n == 0) return HPS_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const unsigned blocks = grid_for(n, kRowThreads, kRowMaxBlocks);
+  mx_by_width(t->dim, [&](auto width) {
+    mx_by_flag(t->view.bf16 != 0, [&](auto bf16) {
+      mx_get<decltype(bf16)::value, decltype(width)::value / 4><<<blocks, kRowThreads, 0, s>>>(t->view, d_keys, n, d_codes, d_scales, d_found_out);
+    });
+  });
+  return launch_ok() ? HPS_OK : HPS_EDEVICE;
+}
+
+hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
+                          const float* d_bias, void* d_out, hps_value_type type, uint64_t stride, void* stream) {
+  if (!mx_dim_ok(dim) || !mx_rows_ok(queries, dim, kMxMaxQueries) || !mx_rows_ok(rows, dim, kMxMaxRows) || !mx_scale_ok(scale) ||
+      (type != HPS_VALUES_F32 && type != HPS_VALUES_BF16) || stride < rows->n || stride > (1ull << 40))
+    return HPS_EINVAL;
+  if (queries->n == 0 || rows->n == 0) return HPS_OK;
+  const bool bf16 = type == HPS_VALUES_BF16;
+  if (!d_out || !mx_aligned(d_out, bf16 ? 2 : 4) || !mx_aligned(d_bias, 4)) return HPS_EINVAL;
+  const uint64_t row_tiles = mx_ceil(rows->n, kMxTile * (kMxThreads / kWave)), blocks = row_tiles * mx_ceil(queries->n, kMxTile);
+  if (blocks > kMxMaxBlocks) return HPS_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  mx_by_width(dim, [&](auto width) {
+    mx_by_flag(d_bias != nullptr, [&](auto biased) {
+      mx_by_flag(bf16, [&](auto narrow) {
+        mx_scores<decltype(width)::value, decltype(biased)::value, decltype(narrow)::value><<<(unsigned)blocks, kMxThreads, 0, s>>>(
+            mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, d_out, stride, (u32)row_tiles);
+      });
+    });
+  });
+  return launch_ok() ? HPS_OK : HPS_EDEVICE;
+}
+
+static bool mx_sizes_ok(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
+  return mx_dim_ok(dim) && n_queries <= kMxMaxQueries && n_rows <= kMxMaxRows;
+}
+
+size_t hps_mx4_logprobs_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top) {
+  if (!mx_sizes_ok(n_queries, n_rows, dim) || top > HPS_MX4_MAX_TOP) return 0;
+  if (n_queries == 0 || n_rows == 0) return kAlign;
+  const MxSplit p = mx_split(n_queries, n_rows, dim, top, kMxWaves);
+  return mx_parts_bytes(p, n_queries) + align_up(p.groups * n_queries * sizeof(float));
+}
+
+hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
+                            const float* d_bias, const int32_t* d_given, uint32_t n_given, uint32_t top,
+                            float* d_lse, float* d_entropy, float* d_logp, int32_t* d_top_index, float* d_top_logp,
+                            void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (!mx_dim_ok(dim) || !mx_rows_ok(queries, dim, kMxMaxQueries) || !mx_rows_ok(rows, dim, kMxMaxRows) || !mx_scale_ok(scale) ||
+      top > HPS_MX4_MAX_TOP || n_given > (1u << 20))
+    return HPS_EINVAL;
+  const uint64_t m = queries->n;
+  if (m == 0) return HPS_OK;
+  if (!d_lse || !d_entropy || (n_given && (!d_given || !d_logp)) || (top && (!d_top_index || !d_top_logp))) return HPS_EINVAL;
+  if (!mx_aligned(d_bias, 4) || !mx_aligned(d_given, 4) || !mx_aligned(d_lse, 4) || !mx_aligned(d_entropy, 4) || !mx_aligned(d_logp, 4) ||
+      !mx_aligned(d_top_index, 4) || !mx_aligned(d_top_logp, 4))
+    return HPS_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (rows->n == 0) {
+    mx_no_rows<<<grid_for(m * std::max(std::max(n_given, top), 1u), kMxThreads, 1u << 16), kMxThreads, 0, s>>>(
+        (u32)m, d_given, n_given, top, d_lse, d_entropy, d_logp, d_top_index, d_top_logp);
+    return launch_ok() ? HPS_OK : HPS_EDEVICE;
+  }
+  if (!d_workspace || !mx_aligned(d_workspace, kAlign)) return HPS_EINVAL;
+  if (workspace_bytes < hps_mx4_logprobs_bytes(m, rows->n, dim, top)) return HPS_ENOMEM;
+  const MxSplit p = mx_split(m, rows->n, dim, top, kMxWaves);
+  MxPart* parts = static_cast<MxPart*>(d_workspace);
+  float* highest = top ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + mx_parts_bytes(p, m)) : nullptr;
+  mx_by_width(dim, [&](auto width) {
+    mx_by_flag(d_bias != nullptr, [&](auto biased) {
+      constexpr int W = decltype(width)::value;
+      constexpr bool B = decltype(biased)::value;
+      mx_softmax<W, B><<<dim3((unsigned)p.parts, (unsigned)p.query_tiles), kWave, 0, s>>>(
+          mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, (u32)p.part_rows, (u32)p.group, (u32)p.groups, parts, highest);
+      mx_finish<W, B><<<(unsigned)m, kMxFinishWaves * kWave, 0, s>>>(
+          mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, parts, (u32)p.parts, highest, (u32)p.group, (u32)p.groups, d_given,
+          n_given, top, d_lse, d_entropy, d_logp, d_top_index, d_top_logp);
+    });
+  });
+  return launch_ok() ? HPS_OK : HPS_EDEVICE;
+}
+
+size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
+  if (!mx_sizes_ok(n_queries, n_rows, dim)) return 0;
+  if (n_queries == 0 || n_rows == 0) return kAlign;
+  return align_up(mx_split(n_queries, n_rows, dim, 0, kMxWaves / 4).parts * n_queries * dim * sizeof(float));
+}
+
+hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
+                                     const float* d_bias, const float* d_lse, const float* d_entropy,
+                                     const int32_t* d_given, const float* d_dlogp, uint32_t n_given,
+                                     const float* d_dentropy, float* d_dqueries, void* d_workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (!mx_dim_ok(dim) || !mx_rows_ok(queries, dim, kMxMaxQueries) || !mx_rows_ok(rows, dim, kMxMaxRows) || !mx_scale_ok(scale) ||
+      n_given > (1u << 20))
+    return HPS_EINVAL;
+  const uint64_t m = queries->n;
+  if (m == 0) return HPS_OK;
+  if (!d_lse || !d_dqueries || (n_given && (!d_given || !d_dlogp)) || (d_dentropy && !d_entropy)) return HPS_EINVAL;
+  if (!mx_aligned(d_bias, 4) || !mx_aligned(d_lse, 4) || !mx_aligned(d_entropy, 4) || !mx_aligned(d_given, 4) || !mx_aligned(d_dlogp, 4) ||
+      !mx_aligned(d_dentropy, 4) || !mx_aligned(d_dqueries, 16) || !d_workspace || !mx_aligned(d_workspace, kAlign))
+    return HPS_EINVAL;
+  if (workspace_bytes < hps_mx4_logprobs_backward_bytes(m, rows->n, dim)) return HPS_ENOMEM;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  MxSplit p = {};
+  float* parts = static_cast<float*>(d_workspace);
+  const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
+  if (rows->n) {
+    p = mx_split(m, rows->n, dim, 0, kMxWaves / 4);
+    mx_by_width(dim, [&](auto width) {
+      mx_by_flag(d_bias != nullptr, [&](auto biased) {
+        mx_gradient<decltype(width)::value, decltype(biased)::value>
+            <<<dim3((unsigned)p.parts, (unsigned)p.query_tiles, (unsigned)mx_ceil(dim, kMxGradColumns)), kMxThreads, 0, s>>>(
+                mx_held(queries), mx_held(rows), dim, blocks, row_bytes, scale, d_bias, d_lse, d_entropy, d_given, d_dlogp, n_given,
+                d_dentropy, (u32)p.part_rows, parts);
+      });
+    });
+  }
+  mx_by_flag(d_bias != nullptr, [&](auto biased) {
+    mx_gradient_end<decltype(biased)::value><<<grid_for(m * dim, kMxThreads, 1u << 16), kMxThreads, 0, s>>>(
+        mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, d_given, d_dlogp, n_given, parts, (u32)p.parts, d_dqueries);
+  });
+  return launch_ok() ? HPS_OK : HPS_EDEVICE;
+}
+
+}  // extern "C"
