@@ -175,45 +175,130 @@ struct MxHeld {            // rows as a kernel sees them
   u32 n;
 };
 
-// Block `block` of row `row` (below n), of 2^-127 zeros where the row has no such block.  WIDTH: bytes of a
-// block (16, or those of a whole narrow row).
+// For kernels that work on products element by element: with at most 256 registers a lane the compiler has the matrix
+// instructions write where other instructions can read, which saves a move each way per element.
+#define HPS_MX_WAVES __attribute__((amdgpu_waves_per_eu(2)))
+
+// How a kernel is made for a width: WIDTH bytes of a block (16, or those of a whole narrow row), and STEPS
+// instructions of 64 values for a product (1, 2, 4, 8 or 16; where a row has fewer, the last ones are skipped).
+template <int WIDTH_, int STEPS_>
+struct MxShape {
+  static constexpr int WIDTH = WIDTH_, STEPS = STEPS_;
+  // words that hold the scale bytes of a lane's blocks, four to a word
+  static constexpr int SCALE_WORDS = (STEPS + 3) / 4;
+};
+
+// One operand of all steps, as lane l holds it: of its row blocks l / 32, 2 + l / 32, ...
+template <typename SHAPE>
+struct MxRow {
+  int4 codes[SHAPE::STEPS];
+  u32 scales[SHAPE::SCALE_WORDS];
+};
+
 template <int WIDTH>
-__device__ __forceinline__ void mx_load(const MxHeld& m, u32 row, u32 block, u32 blocks, MxOperand* codes, u32* scale) {
-  MxOperand c = {0, 0, 0, 0, 0, 0, 0, 0};
-  *scale = 0;
-  if (block < blocks) {
-    if (WIDTH == 16) {
-      const int4 w = *reinterpret_cast<const int4*>(m.codes + ((u64)row * blocks + block) * 16);
-      c[0] = w.x; c[1] = w.y; c[2] = w.z; c[3] = w.w;
-    } else if (WIDTH == 8) {
-      const int2 w = *reinterpret_cast<const int2*>(m.codes + (u64)row * 8);
-      c[0] = w.x; c[1] = w.y;
-    } else {
-      c[0] = *reinterpret_cast<const int*>(m.codes + (u64)row * 4);
-    }
-    *scale = m.scales[(u64)row * blocks + block];
+__device__ __forceinline__ int4 mx_load_block(const uint8_t* at) {
+  if (WIDTH == 16) return *reinterpret_cast<const int4*>(at);
+  if (WIDTH == 8) {
+    const int2 w = *reinterpret_cast<const int2*>(at);
+    return make_int4(w.x, w.y, 0, 0);
   }
-  *codes = c;
+  return make_int4(*reinterpret_cast<const int*>(at), 0, 0, 0);
 }
 
-__device__ __forceinline__ MxTile mx_multiply(const MxOperand& a, u32 a_scale, const MxOperand& b, u32 b_scale, MxTile d) {
-  constexpr int kFp4 = 4;
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, kFp4, kFp4, 0, (int)a_scale, 0, (int)b_scale);
-}
-
-// The products of 32 rows of `a` and 32 of `b`; a_row / b_row: the row that lane l % 32 brings.
-template <int WIDTH>
-__device__ __forceinline__ MxTile mx_products(const MxHeld& a, u32 a_row, const MxHeld& b, u32 b_row, u32 blocks) {
+// Loads a lane's blocks of row `row` (below n).  A block that the row does not have (`blocks` is odd, or below 2 *
+// STEPS - 1) is read as the row's last one: the other operand has to be zero there, which mx_clear_rest sees to.
+template <typename SHAPE>
+__device__ __forceinline__ void mx_load_row(const MxHeld& m, u32 row, u32 blocks, MxRow<SHAPE>* to) {
   const u32 half = lane_id() / 32;
+  if (SHAPE::WIDTH < 16) {
+    to->codes[0] = mx_load_block<SHAPE::WIDTH>(m.codes + (u64)row * SHAPE::WIDTH);
+    to->scales[0] = m.scales[row];
+    return;
+  }
+  const u64 first = (u64)row * blocks;
+#pragma unroll
+  for (int s = 0; s < SHAPE::STEPS; ++s)
+    if (s == 0 || 2 * s < (int)blocks) to->codes[s] = mx_load_block<16>(m.codes + (first + min(2 * s + half, blocks - 1)) * 16);
+  if (SHAPE::STEPS == 1) {
+    to->scales[0] = m.scales[first + min(half, blocks - 1)];
+    return;
+  }
+  // Eight scale bytes at a time, those of four steps of both halves; where fewer are left in the array, the last
+  // eight of it, shifted.
+  const u64 all = (u64)m.n * blocks;
+#pragma unroll
+  for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) {
+    if (8 * w >= (int)blocks) { to->scales[w] = 0; continue; }
+    u64 eight;
+    if (all >= 8) {
+      const u64 at = first + 8 * w, from = min(at, all - 8);
+      __builtin_memcpy(&eight, m.scales + from, 8);
+      eight >>= 8 * (at - from);
+    } else {
+      eight = 0;
+      for (u32 i = 0; i < min(8u, blocks - 8 * w); ++i) eight |= (u64)m.scales[first + 8 * w + i] << (8 * i);
+    }
+    to->scales[w] = __builtin_amdgcn_perm((u32)(eight >> 32), (u32)eight, half ? 0x07050301u : 0x06040200u);
+  }
+  // (the byte behind the last block of an odd number is another row's, and may stand for NaN)
+  if (blocks & 1u) {
+#pragma unroll
+    for (int w = 0; w < SHAPE::SCALE_WORDS; ++w)
+      if (half && blocks / 8 == (u32)w) to->scales[w] &= ~(0xFFu << (8 * (blocks / 2 % 4)));
+  }
+}
+
+// Takes out of an operand what mx_load_row has read in place of blocks that the rows do not have.
+template <typename SHAPE>
+__device__ __forceinline__ void mx_clear_rest(u32 blocks, MxRow<SHAPE>* row) {
+  const u32 half = lane_id() / 32;
+#pragma unroll
+  for (int s = 0; s < SHAPE::STEPS; ++s)
+    if (2 * s + half >= blocks) row->codes[s] = make_int4(0, 0, 0, 0);
+}
+
+template <int STEP>
+__device__ __forceinline__ MxTile mx_step(int4 a, u32 a_scales, int4 b, u32 b_scales, MxTile d) {
+  constexpr int kFp4 = 4;
+  const MxOperand wa = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, wb = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, wb, d, kFp4, kFp4, STEP % 4, (int)a_scales, STEP % 4, (int)b_scales);
+}
+
+template <typename SHAPE, int STEP = 0>
+__device__ __forceinline__ void mx_steps(const MxRow<SHAPE>& a, const MxRow<SHAPE>& b, u32 blocks, MxTile* d) {
+  if constexpr (STEP < SHAPE::STEPS) {
+    if (STEP == 0 || 2 * STEP < (int)blocks) *d = mx_step<STEP>(a.codes[STEP], a.scales[STEP / 4], b.codes[STEP], b.scales[STEP / 4], *d);
+    mx_steps<SHAPE, STEP + 1>(a, b, blocks, d);
+  }
+}
+
+__device__ __forceinline__ MxTile mx_zero_tile() {
   MxTile d;
 #pragma unroll
   for (int r = 0; r < 16; ++r) d[r] = 0.f;
+  return d;
+}
+
+// The products of 32 rows with 32 others; one of the two without what lies behind a row's blocks.
+template <typename SHAPE>
+__device__ __forceinline__ MxTile mx_products(const MxRow<SHAPE>& a, const MxRow<SHAPE>& b, u32 blocks) {
+  MxTile d = mx_zero_tile();
+  mx_steps<SHAPE>(a, b, blocks, &d);
+  return d;
+}
+
+// The same step by step, for rows that a wave meets once: nothing is held between the steps.
+template <int WIDTH>
+__device__ __forceinline__ MxTile mx_products_once(const MxHeld& a, u32 a_row, const MxHeld& b, u32 b_row, u32 blocks) {
+  const u32 half = lane_id() / 32;
+  MxTile d = mx_zero_tile();
+#pragma unroll 4
   for (u32 s = 0; s < blocks; s += 2) {
-    MxOperand ca, cb;
-    u32 sa, sb;
-    mx_load<WIDTH>(a, a_row, s + half, blocks, &ca, &sa);
-    mx_load<WIDTH>(b, b_row, s + half, blocks, &cb, &sb);
-    d = mx_multiply(ca, sa, cb, sb, d);
+    const u32 block = min(s + half, blocks - 1);
+    const int4 ca = mx_load_block<WIDTH>(a.codes + ((u64)a_row * blocks + block) * WIDTH);
+    int4 cb = mx_load_block<WIDTH>(b.codes + ((u64)b_row * blocks + block) * WIDTH);
+    if (s + half >= blocks) cb = make_int4(0, 0, 0, 0);
+    d = mx_step<0>(ca, a.scales[(u64)a_row * blocks + block], cb, b.scales[(u64)b_row * blocks + block], d);
   }
   return d;
 }

@@ -46,7 +46,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   for (u32 row0 = first; row0 < end; row0 += kMxTile) {
     __syncthreads();
     if (wave == 0) {
-      const MxTile d = mx_products<WIDTH>(rows, min(row0 + lane % 32, rows.n - 1), queries, mine, blocks);
+      const MxTile d = mx_products_once<WIDTH>(rows, min(row0 + lane % 32, rows.n - 1), queries, mine, blocks);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const u32 i = mx_row_of(r, half), row = row0 + i;

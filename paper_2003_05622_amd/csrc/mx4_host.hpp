@@ -19,24 +19,31 @@ MxHeld mx_held(const hps_mx4_rows* r) { return {r->d_codes, r->d_scales, (u32)r-
 
 uint64_t mx_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// How the rows are dealt out over the waves: so many parts that the GPU is full.
+// How the rows are dealt out over the waves: so many parts that the GPU is full, a multiple of 8, so that all waves of
+// a part share an XCD and with it the L2 that holds its rows.
 constexpr uint64_t kMxWaves = 4096;
+constexpr uint64_t kMxFewQueries = 256;
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
 };
-MxSplit mx_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top, uint64_t waves) {
+// Query tiles a wave of mx_softmax holds: two share what is read of the rows.
+int mx_wave_tiles(uint64_t n_queries, uint32_t dim) { return n_queries > kMxTile && mx_blocks(dim) <= 8 ? 2 : 1; }
+MxSplit mx_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top, uint32_t wave_tiles, uint64_t waves) {
   MxSplit s;
-  s.query_tiles = mx_ceil(n_queries, kMxTile);
+  s.query_tiles = mx_ceil(n_queries, kMxTile * wave_tiles);
   // rows of a group: what noting the groups' highest scores costs (4 bytes a group, written and read) against scoring the rows of
   // `top` groups once more
   s.group = kMxTile;
   const double row = mx_row_bytes(dim) + mx_blocks(dim);
   while (top && s.group < 1024 && 8.0 * n_rows / (double)s.group > (double)top * (double)(2 * s.group) * row) s.group *= 2;
-  const uint64_t wanted = std::max<uint64_t>(1, waves / s.query_tiles);
+  const uint64_t wanted = mx_ceil(std::max<uint64_t>(1, waves / s.query_tiles), kXcds) * kXcds;
   s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), s.group) * s.group;
   s.parts = mx_ceil(n_rows, s.part_rows);
   s.groups = top ? mx_ceil(n_rows, s.group) : 0;
   return s;
+}
+MxSplit mx_softmax_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top) {
+  return mx_split(n_queries, n_rows, dim, top, (uint32_t)mx_wave_tiles(n_queries, dim), kMxWaves);
 }
 size_t mx_parts_bytes(const MxSplit& s, uint64_t n_queries) { return align_up(s.parts * n_queries * sizeof(MxPart)); }
 
@@ -47,12 +54,23 @@ void mx_by_width(uint32_t dim, F f) {
   else f(std::integral_constant<int, 16>());
 }
 template <typename F>
+void mx_by_shape(uint32_t dim, F f) {
+  const uint32_t blocks = mx_blocks(dim);
+  if (dim <= 8) f(MxShape<4, 1>());
+  else if (dim <= 16) f(MxShape<8, 1>());
+  else if (blocks <= 2) f(MxShape<16, 1>());
+  else if (blocks <= 4) f(MxShape<16, 2>());
+  else if (blocks <= 8) f(MxShape<16, 4>());
+  else if (blocks <= 16) f(MxShape<16, 8>());
+  else f(MxShape<16, 16>());
+}
+template <typename F>
 void mx_by_flag(bool flag, F f) {
   if (flag) f(std::true_type());
   else f(std::false_type());
 }
 
-bool mx_scale_ok(float scale) { return scale - scale == 0.f; }     // (finite)
+bool mx_scale_ok(float scale) { return scale >= -0x1p100f && scale <= 0x1p100f; }
 
 }  // namespace
 
@@ -132,7 +150,7 @@ static bool mx_sizes_ok(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
 size_t hps_mx4_logprobs_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top) {
   if (!mx_sizes_ok(n_queries, n_rows, dim) || top > HPS_MX4_MAX_TOP) return 0;
   if (n_queries == 0 || n_rows == 0) return kAlign;
-  const MxSplit p = mx_split(n_queries, n_rows, dim, top, kMxWaves);
+  const MxSplit p = mx_softmax_split(n_queries, n_rows, dim, top);
   return mx_parts_bytes(p, n_queries) + align_up(p.groups * n_queries * sizeof(float));
 }
 
@@ -157,18 +175,33 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
   }
   if (!d_workspace || !mx_aligned(d_workspace, kAlign)) return HPS_EINVAL;
   if (workspace_bytes < hps_mx4_logprobs_bytes(m, rows->n, dim, top)) return HPS_ENOMEM;
-  const MxSplit p = mx_split(m, rows->n, dim, top, kMxWaves);
+  const MxSplit p = mx_softmax_split(m, rows->n, dim, top);
   MxPart* parts = static_cast<MxPart*>(d_workspace);
   float* highest = top ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + mx_parts_bytes(p, m)) : nullptr;
-  mx_by_width(dim, [&](auto width) {
-    mx_by_flag(d_bias != nullptr, [&](auto biased) {
+  mx_by_flag(d_bias != nullptr, [&](auto biased) {
+    constexpr bool B = decltype(biased)::value;
+    const dim3 grid((unsigned)p.parts, (unsigned)p.query_tiles);
+    mx_by_shape(dim, [&](auto shape) {
+      typedef decltype(shape) Shape;
+#define HPS_MX_SOFTMAX(QT)                                                                                                   \
+  mx_softmax<Shape, B, QT><<<grid, kWave, 0, s>>>(mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias,            \
+                                                  (u32)p.part_rows, (u32)p.group, (u32)p.groups, parts, highest)
+      if constexpr (Shape::STEPS <= 4) {
+        if (mx_wave_tiles(m, dim) == 2) { HPS_MX_SOFTMAX(2); return; }
+      }
+      HPS_MX_SOFTMAX(1);
+#undef HPS_MX_SOFTMAX
+    });
+    mx_by_width(dim, [&](auto width) {
       constexpr int W = decltype(width)::value;
-      constexpr bool B = decltype(biased)::value;
-      mx_softmax<W, B><<<dim3((unsigned)p.parts, (unsigned)p.query_tiles), kWave, 0, s>>>(
-          mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, (u32)p.part_rows, (u32)p.group, (u32)p.groups, parts, highest);
-      mx_finish<W, B><<<(unsigned)m, kMxFinishWaves * kWave, 0, s>>>(
-          mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, parts, (u32)p.parts, highest, (u32)p.group, (u32)p.groups, d_given,
-          n_given, top, d_lse, d_entropy, d_logp, d_top_index, d_top_logp);
+#define HPS_MX_FINISH(WAVES)                                                                                                 \
+  mx_finish<W, B, WAVES><<<(unsigned)m, WAVES * kWave, 0, s>>>(                                                              \
+      mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, parts, (u32)p.parts, highest, (u32)p.group,            \
+      (u32)p.groups, d_given, n_given, top, d_lse, d_entropy, d_logp, d_top_index, d_top_logp)
+      // (few queries leave the GPU idle: then a query's work is spread further)
+      if (m <= kMxFewQueries) HPS_MX_FINISH(16);
+      else HPS_MX_FINISH(4);
+#undef HPS_MX_FINISH
     });
   });
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
@@ -177,7 +210,7 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
 size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
   if (!mx_sizes_ok(n_queries, n_rows, dim)) return 0;
   if (n_queries == 0 || n_rows == 0) return kAlign;
-  return align_up(mx_split(n_queries, n_rows, dim, 0, kMxWaves / 4).parts * n_queries * dim * sizeof(float));
+  return align_up(mx_split(n_queries, n_rows, dim, 0, 1, kMxWaves / 4).parts * n_queries * dim * sizeof(float));
 }
 
 hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
@@ -200,7 +233,7 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
   float* parts = static_cast<float*>(d_workspace);
   const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
   if (rows->n) {
-    p = mx_split(m, rows->n, dim, 0, kMxWaves / 4);
+    p = mx_split(m, rows->n, dim, 0, 1, kMxWaves / 4);
     mx_by_width(dim, [&](auto width) {
       mx_by_flag(d_bias != nullptr, [&](auto biased) {
         mx_gradient<decltype(width)::value, decltype(biased)::value>

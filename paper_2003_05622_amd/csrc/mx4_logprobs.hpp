@@ -20,71 +20,165 @@ constexpr float kMxLog2e = 1.44269504088896340736f;
 constexpr float kMxLn2 = 0.69314718055994530942f;
 constexpr float kMxInf = __builtin_huge_valf();
 
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }     // (2^x below 2^-126 is 0)
 
-struct MxPart {        // what a part of the rows adds to a query, m in scores
+// What some rows add to a query.  m and the exponents behind l and e are in products (of a biased query: in scores), times
+// `unit` they are in powers of two: l = sum 2^((x - m) unit), e = sum 2^((x - m) unit) (x - m) unit.
+struct MxPart {
   float m, l, e;
 };
-__device__ __forceinline__ MxPart mx_no_part() { return {-3.402823466e38f, 0.f, 0.f}; }
-__device__ __forceinline__ MxPart mx_join(const MxPart& a, const MxPart& b) {
+constexpr float kMxLowest = -3.402823466e38f;
+__device__ __forceinline__ MxPart mx_no_part() { return {kMxLowest, 0.f, 0.f}; }
+// Brings a part to a higher m.
+__device__ __forceinline__ void mx_raise(MxPart* a, float m, float unit) {
+  const float by = (a->m - m) * unit, f = exp2f(by);
+  a->e = f == 0.f ? 0.f : (a->e + a->l * by) * f;       // (`by` may be too large to multiply with)
+  a->l *= f;
+  a->m = m;
+}
+__device__ __forceinline__ MxPart mx_join(MxPart a, MxPart b, float unit) {
   const float m = fmaxf(a.m, b.m);
-  MxPart s = {m, 0.f, 0.f};
-  // (a part without rows adds nothing, whatever its m)
-  if (a.l != 0.f) {
-    const float d = a.m - m, f = expf(d);
-    s.l += a.l * f;
-    s.e += f == 0.f ? 0.f : (a.e + a.l * d) * f;
-  }
-  if (b.l != 0.f) {
-    const float d = b.m - m, f = expf(d);
-    s.l += b.l * f;
-    s.e += f == 0.f ? 0.f : (b.e + b.l * d) * f;
-  }
-  return s;
+  mx_raise(&a, m, unit);
+  mx_raise(&b, m, unit);
+  return {m, a.l + b.l, a.e + b.e};
+}
+__device__ __forceinline__ MxPart mx_shuffle_xor(MxPart a, int distance) {
+  return {__shfl_xor(a.m, distance, kWave), __shfl_xor(a.l, distance, kWave), __shfl_xor(a.e, distance, kWave)};
 }
 
-template <int WIDTH, bool BIAS>
-__global__ void __launch_bounds__(kWave)
+// Adds 16 rows' products d to a query's sums.  MASKED: only rows i (of the tile) below `rows` are there.
+template <bool BIAS, bool MASKED>
+__device__ __forceinline__ void mx_add_rows(const MxTile& d, float scale, const float* bias, u32 rows, float unit, MxPart* sum, float* high) {
+  const u32 half = lane_id() / 32;
+  float x[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    x[r] = BIAS ? __fmaf_rn(d[r], scale, bias[r]) : d[r];
+    if (MASKED && mx_row_of(r, half) >= rows) x[r] = -kMxInf;
+  }
+  float most[8];
+#pragma unroll
+  for (int r = 0; r < 5; ++r) most[r] = fmaxf(fmaxf(x[3 * r], x[3 * r + 1]), x[3 * r + 2]);
+  most[0] = fmaxf(fmaxf(most[0], most[1]), most[2]);
+  most[3] = fmaxf(fmaxf(most[3], most[4]), x[15]);
+  most[0] = fmaxf(most[0], most[3]);
+  *high = fmaxf(*high, most[0]);
+  // (seldom, once a wave has seen some rows)
+  if (__any(most[0] > sum->m)) {
+    const float m = fmaxf(sum->m, most[0]), by = (sum->m - m) * unit, f = exp2_fast(by);
+    sum->e = f == 0.f ? 0.f : (sum->e + sum->l * by) * f;
+    sum->l *= f;
+    sum->m = m;
+  }
+  // Rows that are out: 2^-inf.  A biased exponent may be below all numbers, and is not multiplied with then.
+  const float base = -sum->m * unit;
+  float l[16], e[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    float t = BIAS ? (x[r] - sum->m) * unit : __fmaf_rn(x[r], unit, base);
+    if (MASKED && !BIAS && mx_row_of(r, half) >= rows) t = -kMxInf;
+    l[r] = exp2_fast(t);
+    e[r] = BIAS || MASKED ? fmaxf(t, -1e30f) : t;
+  }
+  // (added up among themselves first: 16 times fewer additions onto the long sums)
+  float e0 = 0.f, e1 = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {
+    e0 = __fmaf_rn(l[r], e[r], e0);
+    e1 = __fmaf_rn(l[r + 1], e[r + 1], e1);
+  }
+  sum->e += e0 + e1;
+#pragma unroll
+  for (int w = 8; w; w /= 2)
+#pragma unroll
+    for (int r = 0; r < w; ++r) l[r] += l[r + w];
+  sum->l += l[0];
+}
+
+// A wave, QT * 32 queries, one part of the rows.
+template <typename SHAPE, bool BIAS, int QT>
+__global__ void __launch_bounds__(kWave) HPS_MX_WAVES
 mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, u32 part_rows, u32 group,
            u32 n_groups, MxPart* __restrict__ parts, float* __restrict__ highest) {
-  const u32 lane = lane_id(), half = lane / 32;
-  const u32 query = blockIdx.y * kMxTile + lane % 32, part = blockIdx.x;
-  const u32 q = min(query, queries.n - 1);
+  __shared__ float s_bias[kMxTile];
+  const u32 lane = lane_id(), half = lane / 32, part = blockIdx.x;
+  const u32 query0 = blockIdx.y * (QT * kMxTile) + lane % 32;
   const u32 first = part * part_rows, end = min(rows.n - first, part_rows) + first;
-  MxPart sum = mx_no_part();
-  float high = -kMxInf;
+  // without a bias the maximum is taken of the products themselves: a negative scale goes into the queries' signs
+  const float unit = BIAS ? kMxLog2e : fabsf(scale) * kMxLog2e;
+  MxRow<SHAPE> q[QT];
+  MxPart sum[QT];
+  float high[QT];
+#pragma unroll
+  for (int k = 0; k < QT; ++k) {
+    mx_load_row<SHAPE>(queries, min(query0 + k * kMxTile, queries.n - 1), blocks, &q[k]);
+    mx_clear_rest<SHAPE>(blocks, &q[k]);
+    if (!BIAS && scale < 0.f) {
+#pragma unroll
+      for (int s = 0; s < SHAPE::STEPS; ++s) {
+        int4& c = q[k].codes[s];
+        c = make_int4(c.x ^ 0x88888888, c.y ^ 0x88888888, c.z ^ 0x88888888, c.w ^ 0x88888888);
+      }
+    }
+    sum[k] = mx_no_part();
+    high[k] = -kMxInf;
+  }
+  MxRow<SHAPE> next;
+  float next_bias = 0.f;
+  mx_load_row<SHAPE>(rows, min(first + lane % 32, rows.n - 1), blocks, &next);
+  if (BIAS) next_bias = mx_bias(bias, min(first + lane % 32, rows.n - 1));
+  u32 in_group = 0;
   for (u32 row0 = first; row0 < end; row0 += kMxTile) {
-    const MxTile d = mx_products<WIDTH>(rows, min(row0 + lane % 32, rows.n - 1), queries, q, blocks);
-    float s[16], most = -kMxInf;
+    MxRow<SHAPE> r = next;
+    const float my_bias = row0 + lane % 32 < end ? next_bias : -kMxInf;
+    const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
+    mx_load_row<SHAPE>(rows, ahead, blocks, &next);
+    float b[16] = {};
+    if (BIAS) {
+      next_bias = mx_bias(bias, ahead);
+      // a row that is out has products all the same, but none that are NaN
+      if (my_bias == -kMxInf) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const u32 row = row0 + mx_row_of(r, half);
-      s[r] = row < end ? mx_score<BIAS>(d[r], scale, BIAS ? mx_bias(bias, row) : 0.f) : -kMxInf;
-      most = fmaxf(most, s[r]);
-    }
-    high = fmaxf(high, most);
-    const float m = fmaxf(sum.m, most);
-    if (sum.l != 0.f) {
-      const float by = sum.m - m, f = exp2_fast(by * kMxLog2e);
-      sum.e = f == 0.f ? 0.f : (sum.e + sum.l * by) * f;
-      sum.l *= f;
-    }
-    sum.m = m;
+        for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r.scales[w] = 0;
+      }
+      __builtin_amdgcn_wave_barrier();
+      s_bias[lane % 32] = my_bias;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float t = s[r] - m, p = exp2_fast(t * kMxLog2e);
-      sum.l += p;
-      sum.e += p * fmaxf(t, -1e30f);
+      for (int g = 0; g < 4; ++g) {
+        const float4 v = *reinterpret_cast<const float4*>(&s_bias[8 * g + 4 * half]);
+        b[4 * g] = v.x; b[4 * g + 1] = v.y; b[4 * g + 2] = v.z; b[4 * g + 3] = v.w;
+      }
     }
-    if (highest && ((row0 - first + kMxTile) % group == 0 || row0 + kMxTile >= end)) {
-      high = fmaxf(high, __shfl_xor(high, 32, kWave));
-      if (half == 0 && query < queries.n) highest[(u64)query * n_groups + row0 / group] = high;
-      high = -kMxInf;
+    MxTile d[QT];
+#pragma unroll
+    for (int k = 0; k < QT; ++k) d[k] = mx_products<SHAPE>(r, q[k], blocks);
+    if (BIAS || row0 + kMxTile <= end) {
+#pragma unroll
+      for (int k = 0; k < QT; ++k) mx_add_rows<BIAS, false>(d[k], scale, b, 0, unit, &sum[k], &high[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < QT; ++k) mx_add_rows<BIAS, true>(d[k], scale, b, end - row0, unit, &sum[k], &high[k]);
+    }
+    in_group += kMxTile;
+    if (highest && (in_group == group || row0 + kMxTile >= end)) {
+      in_group = 0;
+#pragma unroll
+      for (int k = 0; k < QT; ++k) {
+        const float h = fmaxf(high[k], __shfl_xor(high[k], 32, kWave));
+        const u32 query = query0 + k * kMxTile;
+        if (half == 0 && query < queries.n) highest[(u64)query * n_groups + row0 / group] = h;
+        high[k] = -kMxInf;
+      }
     }
   }
-  const MxPart other = {__shfl_xor(sum.m, 32, kWave), __shfl_xor(sum.l, 32, kWave), __shfl_xor(sum.e, 32, kWave)};
-  sum = mx_join(sum, other);
-  if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum;
+#pragma unroll
+  for (int k = 0; k < QT; ++k) {
+    sum[k] = mx_join(sum[k], mx_shuffle_xor(sum[k], 32), unit);
+    const u32 query = query0 + k * kMxTile;
+    if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum[k];
+  }
 }
 
 // ---- the best of many, 64 at a time -----------------------------------------------------------
@@ -100,121 +194,169 @@ __device__ __forceinline__ float mx_candidate_score(u64 c) {
 }
 __device__ __forceinline__ u32 mx_candidate_number(u64 c) { return ~(u32)c; }
 
-__device__ __forceinline__ u64 mx_exchange(u64 c, u32 distance, bool larger) {
-  const u64 o = __shfl_xor((unsigned long long)c, (int)distance, kWave);
+// The value of lane l ^ D, by moves between lanes (a shuffle through the LDS takes some hundred cycles, and a sort has 21).
+template <int D>
+__device__ __forceinline__ u32 mx_lane_xor(u32 v) {
+  static_assert(D == 1 || D == 2 || D == 4 || D == 8 || D == 16 || D == 32, "");
+  if constexpr (D == 1) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);
+  if constexpr (D == 2) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);
+  // (the lanes of eight, and then of each four, backwards)
+  if constexpr (D == 4) return (u32)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
+  if constexpr (D == 8) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);
+  if constexpr (D == 16) {
+    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane_id() & 16u ? both[0] : both[1];
+  }
+  if constexpr (D == 32) {
+    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane_id() & 32u ? both[0] : both[1];
+  }
+}
+template <int D>
+__device__ __forceinline__ u64 mx_exchange(u64 c, bool larger) {
+  const u64 o = (u64)mx_lane_xor<D>((u32)(c >> 32)) << 32 | mx_lane_xor<D>((u32)c);
   return (o > c) == larger ? o : c;
+}
+template <int RUN, int D>
+__device__ __forceinline__ u64 mx_sort_run(u64 c) {
+  if constexpr (D >= 1) {
+    const u32 lane = lane_id();
+    c = mx_exchange<D>(c, ((lane & RUN) == 0) == ((lane & D) == 0));
+    c = mx_sort_run<RUN, D / 2>(c);
+  }
+  return c;
 }
 // Lane i gets the i-th largest of the wave's 64 candidates.
 __device__ __forceinline__ u64 mx_sort(u64 c) {
-  const u32 lane = lane_id();
-#pragma unroll
-  for (u32 run = 2; run <= 64; run *= 2)
-#pragma unroll
-    for (u32 d = run / 2; d; d /= 2) c = mx_exchange(c, d, ((lane & run) == 0) == ((lane & d) == 0));
-  return c;
+  c = mx_sort_run<2, 1>(c);
+  c = mx_sort_run<4, 2>(c);
+  c = mx_sort_run<8, 4>(c);
+  c = mx_sort_run<16, 8>(c);
+  c = mx_sort_run<32, 16>(c);
+  return mx_sort_run<64, 32>(c);
+}
+__device__ __forceinline__ u32 mx_lane_reversed(u32 v) {
+  return mx_lane_xor<32>(mx_lane_xor<16>((u32)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true)));
 }
 // Of two lists in descending order the 64 largest, in descending order.
 __device__ __forceinline__ u64 mx_merge(u64 a, u64 b) {
-  const u32 lane = lane_id();
-  const u64 r = __shfl((unsigned long long)b, 63 - (int)lane, kWave);
-  u64 c = a > r ? a : r;
-#pragma unroll
-  for (u32 d = 32; d; d /= 2) c = mx_exchange(c, d, (lane & d) == 0);
-  return c;
+  const u64 r = (u64)mx_lane_reversed((u32)(b >> 32)) << 32 | mx_lane_reversed((u32)b);
+  return mx_sort_run<64, 32>(a > r ? a : r);
 }
 // Adds 64 candidates to a list of which the first `top` count.
 __device__ __forceinline__ void mx_offer(u64* list, u64 c, u32 top) {
-  const u64 least = __shfl((unsigned long long)*list, (int)top - 1, kWave);
+  const u64 least = wave_lane(*list, (int)top - 1);
   if (__any(c > least)) *list = mx_merge(*list, mx_sort(c));
 }
-
-constexpr int kMxFinishWaves = 4;
+// Joins the lists of a workgroup's waves in s_list[0].
+template <int WAVES>
+__device__ __forceinline__ void mx_join_lists(u64 (*s_list)[kWave], u64 list) {
+  const u32 lane = lane_id(), wave = threadIdx.x / kWave;
+  s_list[wave][lane] = list;
+#pragma unroll
+  for (u32 d = 1; d < WAVES; d *= 2) {
+    __syncthreads();
+    if (wave % (2 * d) == 0) s_list[wave][lane] = list = mx_merge(list, s_list[wave + d][lane]);
+  }
+  __syncthreads();
+}
 
 // The product of one query with the row each lane names (below n).
 template <int WIDTH>
 __device__ __forceinline__ float mx_dots(const MxHeld& queries, u32 query, const MxHeld& rows, u32 row, u32 blocks) {
-  const u32 lane = lane_id();
-  const u32 low = (u32)__shfl((int)row, (int)(lane % 32), kWave), high = (u32)__shfl((int)row, (int)(lane % 32 + 32), kWave);
-  const MxTile a = mx_products<WIDTH>(queries, query, rows, low, blocks);
-  const MxTile b = mx_products<WIDTH>(queries, query, rows, high, blocks);
+  const u32 lane = lane_id(), other = mx_lane_xor<32>(row);
+  const MxTile a = mx_products_once<WIDTH>(queries, query, rows, lane < 32 ? row : other, blocks);
+  const MxTile b = mx_products_once<WIDTH>(queries, query, rows, lane < 32 ? other : row, blocks);
   return lane < 32 ? a[0] : b[0];
 }
 
-template <int WIDTH, bool BIAS>
-__global__ void __launch_bounds__(kMxFinishWaves * kWave)
+// The best groups of a query are found in two turns: every thread takes the best of the groups that fall to it, the best threads are
+// found, and among their groups the best ones (as with rows and groups: the best `top` are among those of the `top` best threads).
+template <int WIDTH, bool BIAS, int WAVES>
+__global__ void __launch_bounds__(WAVES * kWave) HPS_MX_WAVES
 mx_finish(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, const MxPart* __restrict__ parts,
           u32 n_parts, const float* __restrict__ highest, u32 group, u32 n_groups, const i32* __restrict__ given, u32 n_given,
           u32 top, float* __restrict__ lse_out, float* __restrict__ entropy_out, float* __restrict__ logp_out,
           i32* __restrict__ top_index, float* __restrict__ top_logp) {
-  __shared__ u64 s_list[kMxFinishWaves][kWave];
-  __shared__ MxPart s_part[kMxFinishWaves];
+  constexpr u32 kThreads = WAVES * kWave;
+  __shared__ u64 s_list[WAVES][kWave];
+  __shared__ MxPart s_part[WAVES];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave, query = blockIdx.x;
-  // join the parts: every wave some, then every wave all waves'
+  const float to_score = BIAS ? 1.f : fabsf(scale), unit = to_score * kMxLog2e;
+  // join the parts
   MxPart sum = mx_no_part();
-  for (u32 i = threadIdx.x; i < n_parts; i += kMxFinishWaves * kWave) sum = mx_join(sum, parts[(u64)query * n_parts + i]);
+  for (u32 i = threadIdx.x; i < n_parts; i += kThreads) sum = mx_join(sum, parts[(u64)query * n_parts + i], unit);
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const MxPart o = {__shfl_xor(sum.m, d, kWave), __shfl_xor(sum.l, d, kWave), __shfl_xor(sum.e, d, kWave)};
-    sum = mx_join(sum, o);
-  }
+  for (int d = 1; d < kWave; d *= 2) sum = mx_join(sum, mx_shuffle_xor(sum, d), unit);
   if (lane == 0) s_part[wave] = sum;
-  u64 best = 0;
+  const float* mine = highest + (u64)query * n_groups;
   if (top) {
-    for (u32 i0 = wave * kWave; i0 < n_groups; i0 += kMxFinishWaves * kWave) {
-      const u32 g = i0 + lane;
-      const float h = g < n_groups ? highest[(u64)query * n_groups + g] : 0.f;
-      mx_offer(&best, g < n_groups ? mx_candidate(h, g) : 0, top);
+    // (a group without a number among its scores has -inf, also where the scale is 0)
+    auto group_candidate = [&](u32 g) {
+      const float h = mine[g];
+      return mx_candidate(BIAS || h == -kMxInf ? h : __fmul_rn(h, to_score), g);
+    };
+    u64 best = 0;
+    for (u32 g = threadIdx.x; g < n_groups; g += kThreads) {
+      const u64 c = group_candidate(g);
+      best = c > best ? c : best;
     }
-    s_list[wave][lane] = best;
+    mx_join_lists<WAVES>(s_list, mx_sort(best));
+    if (n_groups > kThreads) {
+      const u64 threads = s_list[0][lane];
+      __syncthreads();
+      const u32 each = (n_groups + kThreads - 1) / kThreads, n = min(top, kThreads) * each;
+      u64 list = 0;
+      for (u32 i0 = wave * kWave; i0 < n; i0 += kThreads) {
+        const u32 i = i0 + lane, g = mx_candidate_number(__shfl((unsigned long long)threads, (int)min(i / each, 63u), kWave)) % kThreads + i % each * kThreads;
+        mx_offer(&list, i < n && g < n_groups ? group_candidate(g) : 0, top);
+      }
+      mx_join_lists<WAVES>(s_list, list);
+    }
+  } else {
+    __syncthreads();
   }
-  __syncthreads();
   sum = s_part[0];
 #pragma unroll
-  for (int w = 1; w < kMxFinishWaves; ++w) sum = mx_join(sum, s_part[w]);
+  for (int w = 1; w < WAVES; ++w) sum = mx_join(sum, s_part[w], unit);
   const bool empty = sum.l == 0.f;
-  const float lse = empty ? -kMxInf : sum.m + logf(sum.l);
+  const float log2_l = log2f(sum.l), lse = empty ? -kMxInf : __fmaf_rn(log2_l, kMxLn2, sum.m * to_score);
   if (threadIdx.x == 0) {
     lse_out[query] = lse;
-    entropy_out[query] = empty ? 0.f : logf(sum.l) - sum.e / sum.l;
+    entropy_out[query] = empty ? 0.f : (log2_l - sum.e / sum.l) * kMxLn2;
   }
   if (top) {
-    best = s_list[0][lane];
-#pragma unroll
-    for (int w = 1; w < kMxFinishWaves; ++w) best = mx_merge(best, s_list[w][lane]);
+    const u64 groups = s_list[0][lane];
     __syncthreads();
+    // every row that is wanted scores at least as high as the last of `top` groups, each of which has such a row
+    const u32 n_best = min(top, n_groups), each = (group + kWave - 1) / kWave;
+    const u64 last = wave_lane(groups, (int)n_best - 1);
+    const float least = n_best < top ? -kMxInf : mx_candidate_score(last);
     u64 list = 0;
-    for (u32 i = wave; i < top; i += kMxFinishWaves) {
-      const u64 c = __shfl((unsigned long long)best, (int)i, kWave);
-      if (c == 0) break;
-      const u32 g = mx_candidate_number(c);
-      for (u32 k = 0; k < group; k += kWave) {
-        const u32 row = g * group + k + lane;
-        const bool in = k + lane < group && row < rows.n;
-        const u32 at = in ? row : rows.n - 1;
-        const float dot = mx_dots<WIDTH>(queries, query, rows, at, blocks);
-        const float s = mx_score<BIAS>(dot, scale, BIAS ? mx_bias(bias, at) : 0.f);
-        // (a NaN and a row taken out are no candidates)
-        mx_offer(&list, in && s > -kMxInf ? mx_candidate(s, row) : 0, top);
-      }
+    for (u32 i = wave; i < n_best * each; i += WAVES) {
+      const u32 g = mx_candidate_number(wave_lane(groups, (int)(i / each)));
+      const u32 k = i % each * kWave + lane, row = g * group + k;
+      const bool in = k < group && row < rows.n;
+      const u32 at = in ? row : rows.n - 1;
+      const float s = mx_score<BIAS>(mx_dots<WIDTH>(queries, query, rows, at, blocks), scale, BIAS ? mx_bias(bias, at) : 0.f);
+      // (a NaN and a row taken out are no candidates)
+      mx_offer(&list, in && s >= least && s > -kMxInf ? mx_candidate(s, row) : 0, top);
     }
-    s_list[wave][lane] = list;
-    __syncthreads();
+    mx_join_lists<WAVES>(s_list, list);
     if (wave == 0) {
-#pragma unroll
-      for (int w = 1; w < kMxFinishWaves; ++w) list = mx_merge(list, s_list[w][lane]);
+      list = s_list[0][lane];
       if (lane < top) {
         top_index[(u64)query * top + lane] = list ? (i32)mx_candidate_number(list) : -1;
         top_logp[(u64)query * top + lane] = list ? mx_candidate_score(list) - lse : -kMxInf;
       }
     }
   }
-  for (u32 i0 = wave * kWave; i0 < n_given; i0 += kMxFinishWaves * kWave) {
+  for (u32 i0 = wave * kWave; i0 < n_given; i0 += kThreads) {
     const u32 i = i0 + lane;
     const i32 g = i < n_given ? given[(u64)query * n_given + i] : -1;
     const bool in = g >= 0 && (u32)g < rows.n;
     const u32 at = in ? (u32)g : rows.n - 1;
-    const float dot = mx_dots<WIDTH>(queries, query, rows, at, blocks);
-    const float s = mx_score<BIAS>(dot, scale, BIAS ? mx_bias(bias, at) : 0.f);
+    const float s = mx_score<BIAS>(mx_dots<WIDTH>(queries, query, rows, at, blocks), scale, BIAS ? mx_bias(bias, at) : 0.f);
     if (i < n_given)
       logp_out[(u64)query * n_given + i] = g < 0 ? 0.f : !in ? __uint_as_float(0x7FC00000u) : s == -kMxInf ? s : s - lse;
   }

@@ -16,7 +16,7 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
   const u32 row_tile = blockIdx.x % row_tiles, query_tile = blockIdx.x / row_tiles;
   const u32 row = (row_tile * (kMxThreads / kWave) + wave) * kMxTile + lane % 32, query0 = query_tile * kMxTile;
   if (row - lane % 32 >= rows.n) return;
-  const MxTile d = mx_products<WIDTH>(queries, min(query0 + lane % 32, queries.n - 1), rows, min(row, rows.n - 1), blocks);
+  const MxTile d = mx_products_once<WIDTH>(queries, min(query0 + lane % 32, queries.n - 1), rows, min(row, rows.n - 1), blocks);
   if (row >= rows.n) return;
   const float b = BIAS ? mx_bias(bias, row) : 0.f;
 #pragma unroll
