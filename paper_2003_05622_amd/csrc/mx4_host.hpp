@@ -26,8 +26,11 @@ constexpr uint64_t kMxFewQueries = 256;
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
 };
-// Query tiles a wave of mx_softmax holds: two share what is read of the rows.
-int mx_wave_tiles(uint64_t n_queries, uint32_t dim) { return n_queries > kMxTile && mx_blocks(dim) <= 8 ? 2 : 1; }
+// Query tiles a wave of mx_softmax holds: two share what is read of the rows, unless that leaves much of the last ones empty.
+int mx_wave_tiles(uint64_t n_queries, uint32_t dim) {
+  const uint64_t tiles = mx_ceil(n_queries, kMxTile);
+  return mx_blocks(dim) <= 8 && (tiles % 2 == 0 || tiles > 8) ? 2 : 1;
+}
 MxSplit mx_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top, uint32_t wave_tiles, uint64_t waves) {
   MxSplit s;
   s.query_tiles = mx_ceil(n_queries, kMxTile * wave_tiles);

@@ -248,30 +248,55 @@ __device__ __forceinline__ void mx_offer(u64* list, u64 c, u32 top) {
   const u64 least = wave_lane(*list, (int)top - 1);
   if (__any(c > least)) *list = mx_merge(*list, mx_sort(c));
 }
-// Joins the lists of a workgroup's waves in s_list[0].
+// Joins the lists of a workgroup's first `lists` waves in s_list[0].  (A barrier before the next use of s_list.)
 template <int WAVES>
-__device__ __forceinline__ void mx_join_lists(u64 (*s_list)[kWave], u64 list) {
+__device__ __forceinline__ void mx_join_lists(u64 (*s_list)[kWave], u64 list, u32 lists) {
   const u32 lane = lane_id(), wave = threadIdx.x / kWave;
   s_list[wave][lane] = list;
 #pragma unroll
   for (u32 d = 1; d < WAVES; d *= 2) {
+    if (d >= lists) break;
     __syncthreads();
     if (wave % (2 * d) == 0) s_list[wave][lane] = list = mx_merge(list, s_list[wave + d][lane]);
   }
   __syncthreads();
 }
 
-// The product of one query with the row each lane names (below n).
+// Candidates that a workgroup's threads find and that reach a bound, in any order.  Where they are more than there is room
+// for (many equal scores), they are offered to the waves' lists instead, in a second turn.
+template <int WAVES>
+struct MxFound {
+  u64 list[WAVES][kWave];
+  u32 count;
+  __device__ __forceinline__ void add(u64 c) {
+    const u32 at = atomicAdd(&count, 1u);
+    if (at < WAVES * kWave) (&list[0][0])[at] = c;
+  }
+};
+
+// The product of one query with the row each lane names (below n): the rows of the lower lanes and those of the upper ones
+// in an instruction each, with the query in all rows of the other operand.
 template <int WIDTH>
 __device__ __forceinline__ float mx_dots(const MxHeld& queries, u32 query, const MxHeld& rows, u32 row, u32 blocks) {
-  const u32 lane = lane_id(), other = mx_lane_xor<32>(row);
-  const MxTile a = mx_products_once<WIDTH>(queries, query, rows, lane < 32 ? row : other, blocks);
-  const MxTile b = mx_products_once<WIDTH>(queries, query, rows, lane < 32 ? other : row, blocks);
-  return lane < 32 ? a[0] : b[0];
+  const u32 lane = lane_id(), half = lane / 32, other = mx_lane_xor<32>(row);
+  const u64 low = (u64)(half ? other : row) * blocks, high = (u64)(half ? row : other) * blocks, one = (u64)query * blocks;
+  MxTile a = mx_zero_tile(), b = mx_zero_tile();
+#pragma unroll 2
+  for (u32 s = 0; s < blocks; s += 2) {
+    const u32 block = min(s + half, blocks - 1);
+    int4 q = mx_load_block<WIDTH>(queries.codes + (one + block) * WIDTH);
+    const int4 l = mx_load_block<WIDTH>(rows.codes + (low + block) * WIDTH), h = mx_load_block<WIDTH>(rows.codes + (high + block) * WIDTH);
+    const u32 q_scale = queries.scales[one + block], l_scale = rows.scales[low + block], h_scale = rows.scales[high + block];
+    if (s + half >= blocks) q = make_int4(0, 0, 0, 0);
+    a = mx_step<0>(q, q_scale, l, l_scale, a);
+    b = mx_step<0>(q, q_scale, h, h_scale, b);
+  }
+  return half ? b[0] : a[0];
 }
 
-// The best groups of a query are found in two turns: every thread takes the best of the groups that fall to it, the best threads are
-// found, and among their groups the best ones (as with rows and groups: the best `top` are among those of the `top` best threads).
+// The best groups: every thread takes the best of the groups that fall to it, every wave finds its ceil(top / WAVES) best
+// threads; the worst of these, over all waves, is a bound that `top` groups reach, and hardly more than twice as many do.
+// Those that do are collected and sorted.  The rows of the best groups go the same way, with the last group's highest score as the bound.
 template <int WIDTH, bool BIAS, int WAVES>
 __global__ void __launch_bounds__(WAVES * kWave) HPS_MX_WAVES
 mx_finish(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, const MxPart* __restrict__ parts,
@@ -279,46 +304,48 @@ mx_finish(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
           u32 top, float* __restrict__ lse_out, float* __restrict__ entropy_out, float* __restrict__ logp_out,
           i32* __restrict__ top_index, float* __restrict__ top_logp) {
   constexpr u32 kThreads = WAVES * kWave;
-  __shared__ u64 s_list[WAVES][kWave];
+  __shared__ MxFound<WAVES> s_groups, s_rows;
   __shared__ MxPart s_part[WAVES];
+  __shared__ u64 s_bound[WAVES];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave, query = blockIdx.x;
   const float to_score = BIAS ? 1.f : fabsf(scale), unit = to_score * kMxLog2e;
+  const float* mine = highest + (u64)query * n_groups;
+  // (a group without a number among its scores has -inf, also where the scale is 0)
+  auto group_candidate = [&](u32 g) {
+    const float h = mine[g];
+    return mx_candidate(BIAS || h == -kMxInf ? h : __fmul_rn(h, to_score), g);
+  };
+  u64 best = 0;
+  if (threadIdx.x == 0) s_groups.count = s_rows.count = 0;
+  if (top) {
+#pragma unroll 8
+    for (u32 g = threadIdx.x; g < n_groups; g += kThreads) {
+      const u64 c = group_candidate(g);
+      best = c > best ? c : best;
+    }
+    const u64 bound = wave_lane(mx_sort(best), (int)((top + WAVES - 1) / WAVES) - 1);
+    if (lane == 0) s_bound[wave] = bound;
+  }
   // join the parts
   MxPart sum = mx_no_part();
   for (u32 i = threadIdx.x; i < n_parts; i += kThreads) sum = mx_join(sum, parts[(u64)query * n_parts + i], unit);
 #pragma unroll
   for (int d = 1; d < kWave; d *= 2) sum = mx_join(sum, mx_shuffle_xor(sum, d), unit);
   if (lane == 0) s_part[wave] = sum;
-  const float* mine = highest + (u64)query * n_groups;
+  __syncthreads();
   if (top) {
-    // (a group without a number among its scores has -inf, also where the scale is 0)
-    auto group_candidate = [&](u32 g) {
-      const float h = mine[g];
-      return mx_candidate(BIAS || h == -kMxInf ? h : __fmul_rn(h, to_score), g);
-    };
-    u64 best = 0;
-    for (u32 g = threadIdx.x; g < n_groups; g += kThreads) {
-      const u64 c = group_candidate(g);
-      best = c > best ? c : best;
-    }
-    mx_join_lists<WAVES>(s_list, mx_sort(best));
-    if (n_groups > kThreads) {
-      const u64 threads = s_list[0][lane];
-      __syncthreads();
-      const u32 each = (n_groups + kThreads - 1) / kThreads, n = min(top, kThreads) * each;
-      u64 list = 0;
-      for (u32 i0 = wave * kWave; i0 < n; i0 += kThreads) {
-        const u32 i = i0 + lane, g = mx_candidate_number(__shfl((unsigned long long)threads, (int)min(i / each, 63u), kWave)) % kThreads + i % each * kThreads;
-        mx_offer(&list, i < n && g < n_groups ? group_candidate(g) : 0, top);
-      }
-      mx_join_lists<WAVES>(s_list, list);
-    }
-  } else {
-    __syncthreads();
-  }
-  sum = s_part[0];
+    u64 bound = s_bound[0];
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) sum = mx_join(sum, s_part[w], unit);
+    for (int w = 1; w < WAVES; ++w) bound = s_bound[w] < bound ? s_bound[w] : bound;
+    if (best >= bound)
+      for (u32 g = threadIdx.x; g < n_groups; g += kThreads) {
+        const u64 c = group_candidate(g);
+        if (c >= bound) s_groups.add(c);
+      }
+  }
+  sum = s_part[lane % WAVES];
+#pragma unroll
+  for (int d = 1; d < WAVES; d *= 2) sum = mx_join(sum, mx_shuffle_xor(sum, d), unit);
   const bool empty = sum.l == 0.f;
   const float log2_l = log2f(sum.l), lse = empty ? -kMxInf : __fmaf_rn(log2_l, kMxLn2, sum.m * to_score);
   if (threadIdx.x == 0) {
@@ -326,25 +353,47 @@ mx_finish(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
     entropy_out[query] = empty ? 0.f : (log2_l - sum.e / sum.l) * kMxLn2;
   }
   if (top) {
-    const u64 groups = s_list[0][lane];
     __syncthreads();
+    u32 n = s_groups.count;
+    u64 list = 0;
+    if (n <= kThreads) {
+      if (wave * kWave < n) list = mx_sort(threadIdx.x < n ? s_groups.list[wave][lane] : 0);
+    } else {
+      n = kThreads;
+      __syncthreads();
+      for (u32 g0 = wave * kWave; g0 < n_groups; g0 += kThreads) mx_offer(&list, g0 + lane < n_groups ? group_candidate(g0 + lane) : 0, top);
+    }
+    mx_join_lists<WAVES>(s_groups.list, list, (n + kWave - 1) / kWave);
+    const u64 groups = s_groups.list[0][lane];
     // every row that is wanted scores at least as high as the last of `top` groups, each of which has such a row
     const u32 n_best = min(top, n_groups), each = (group + kWave - 1) / kWave;
-    const u64 last = wave_lane(groups, (int)n_best - 1);
-    const float least = n_best < top ? -kMxInf : mx_candidate_score(last);
-    u64 list = 0;
-    for (u32 i = wave; i < n_best * each; i += WAVES) {
+    const float least = n_best < top ? -kMxInf : mx_candidate_score(wave_lane(groups, (int)n_best - 1));
+    // 64 rows, one per lane, of turn i (a NaN and a row taken out are no candidates)
+    auto row_candidate = [&](u32 i) -> u64 {
       const u32 g = mx_candidate_number(wave_lane(groups, (int)(i / each)));
       const u32 k = i % each * kWave + lane, row = g * group + k;
       const bool in = k < group && row < rows.n;
       const u32 at = in ? row : rows.n - 1;
       const float s = mx_score<BIAS>(mx_dots<WIDTH>(queries, query, rows, at, blocks), scale, BIAS ? mx_bias(bias, at) : 0.f);
-      // (a NaN and a row taken out are no candidates)
-      mx_offer(&list, in && s >= least && s > -kMxInf ? mx_candidate(s, row) : 0, top);
+      return in && s >= least && s > -kMxInf ? mx_candidate(s, row) : 0;
+    };
+    for (u32 i = wave; i < n_best * each; i += WAVES) {
+      const u64 c = row_candidate(i);
+      if (c) s_rows.add(c);
     }
-    mx_join_lists<WAVES>(s_list, list);
+    __syncthreads();
+    n = s_rows.count;
+    list = 0;
+    if (n <= kThreads) {
+      if (wave * kWave < n) list = mx_sort(threadIdx.x < n ? s_rows.list[wave][lane] : 0);
+    } else {
+      n = kThreads;
+      __syncthreads();
+      for (u32 i = wave; i < n_best * each; i += WAVES) mx_offer(&list, row_candidate(i), top);
+    }
+    mx_join_lists<WAVES>(s_rows.list, list, (n + kWave - 1) / kWave);
     if (wave == 0) {
-      list = s_list[0][lane];
+      list = s_rows.list[0][lane];
       if (lane < top) {
         top_index[(u64)query * top + lane] = list ? (i32)mx_candidate_number(list) : -1;
         top_logp[(u64)query * top + lane] = list ? mx_candidate_score(list) - lse : -kMxInf;
