@@ -184,6 +184,8 @@ struct MxHeld {            // rows as a kernel sees them
 template <int WIDTH_, int STEPS_>
 struct MxShape {
   static constexpr int WIDTH = WIDTH_, STEPS = STEPS_;
+  // whether the next rows are loaded while the present ones are worked on (wide rows fill the registers by themselves)
+  static constexpr bool AHEAD = STEPS <= 4;
   // words that hold the scale bytes of a lane's blocks, four to a word
   static constexpr int SCALE_WORDS = (STEPS + 3) / 4;
 };

@@ -3,15 +3,27 @@
 // With p_r = exp(s_r - lse), U the sum of the upstream gradients u_g of the given rows' log probabilities
 // and h that of the entropy H:  dL/ds_r = c_r + (u_g where r is given),  c_r = -p_r (U + h (log p_r + H)),
 // d query = scale * (sum_r c_r row_r + sum_g u_g row_g).
-// mx_gradient: a workgroup takes 32 queries, a part of the rows and 64 of the columns; it works c out for 32 rows
-// at a time (as mx_softmax does their scores) and adds c row to its sums.  mx_gradient_end adds the parts and the given rows.
+//
+// mx_gradient goes through the rows once: a product of 32 rows and 32 queries leaves a lane with 16 rows' scores for its
+// query, c of which is at once the second operand of the product with the rows' values (which rows a step of the
+// matrix instruction takes, in which order, is free as long as both operands agree).  The values, exact in
+// bfloat16, are unpacked into LDS by the workgroup, in the order the first operand wants them: lane l of a step holds
+// column l % 32 of eight rows.  c goes through the matrix instruction in three bfloat16 pieces that add up
+// to its 24 bits exactly: the sum over the rows is what little is left of large terms, and eight bits would show.
+// Without a gradient of the entropy c is p up to a factor per query, which the end applies.
+// mx_gradient_end adds the parts of the rows and the given rows.
 #pragma once
 
 #include "mx4_logprobs.hpp"
 
 namespace hps {
 
-constexpr u32 kMxGradColumns = 64;
+constexpr u32 kMxStageTiles = 4;                         // tiles of 32 rows unpacked at a time
+constexpr u32 kMxStageRows = kMxStageTiles * kMxTile;
+constexpr u32 kMxGradWaves = 4;
+
+typedef __bf16 MxHalves2 __attribute__((ext_vector_type(2)));
+typedef __bf16 MxHalves8 __attribute__((ext_vector_type(8)));
 
 // One value of a held row.
 __device__ __forceinline__ float mx_value(const MxHeld& m, u32 row, u32 col, u32 row_bytes, u32 blocks) {
@@ -23,73 +35,253 @@ __device__ __forceinline__ float mx_value(const MxHeld& m, u32 row, u32 col, u32
 template <bool BIAS>
 __device__ __forceinline__ float mx_upstream(const i32* given, const float* d_logp, u64 at, u32 n_rows, const float* bias) {
   const i32 g = given[at];
+  const float u = d_logp[at];
   if (g < 0 || (u32)g >= n_rows) return 0.f;
   if (BIAS && mx_bias(bias, (u32)g) == -kMxInf) return 0.f;
-  return d_logp[at];
+  return u;
 }
 
-template <int WIDTH, bool BIAS>
-__global__ void __launch_bounds__(kMxThreads)
-mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, const float* __restrict__ bias,
-            const float* __restrict__ lse, const float* __restrict__ entropy, const i32* __restrict__ given, const float* __restrict__ d_logp,
-            u32 n_given, const float* __restrict__ d_entropy, u32 part_rows, float* __restrict__ parts) {
-  __shared__ float s_c[kMxTile][kMxTile + 1];
-  __shared__ float s_w[kMxTile][kMxGradColumns];
-  const u32 lane = lane_id(), half = lane / 32, wave = threadIdx.x / kWave;
-  const u32 part = blockIdx.x, query0 = blockIdx.y * kMxTile, col0 = blockIdx.z * kMxGradColumns;
-  const u32 mine = min(query0 + lane % 32, queries.n - 1);
-  float u_all = 0.f;
-  for (u32 g = 0; g < n_given; ++g) u_all += mx_upstream<BIAS>(given, d_logp, (u64)mine * n_given + g, rows.n, bias);
-  const float q_lse = lse[mine], h = d_entropy ? d_entropy[mine] : 0.f, q_entropy = d_entropy ? entropy[mine] : 0.f;
-  float sum[8] = {};
-  const u32 first = part * part_rows, end = min(rows.n - first, part_rows) + first;
-  for (u32 row0 = first; row0 < end; row0 += kMxTile) {
-    __syncthreads();
-    if (wave == 0) {
-      const MxTile d = mx_products_once<WIDTH>(rows, min(row0 + lane % 32, rows.n - 1), queries, mine, blocks);
+// Unpacking: a lane takes eight columns of four neighbouring rows, 8 x COLUMNS / 8 such pieces a tile.
+template <int COLUMNS, bool BIAS>
+struct MxUnpack {
+  static constexpr int PIECES = (COLUMNS + kWave / 8 * 8 - 1) / (kWave / 8 * 8);       // a lane's pieces of a tile
+  u32 codes[PIECES][4];
+  u32 scales[PIECES];                                                                    // a byte each
+  static __device__ __forceinline__ bool place(int piece, u32* quad, u32* word) {
+    const u32 at = piece * kWave + lane_id();
+    *quad = at % 8;
+    *word = at / 8;
+    return *word < COLUMNS / 8;
+  }
+  __device__ __forceinline__ void load(const MxHeld& rows, u32 row0, u32 end, u32 col0, u32 row_bytes, u32 blocks, const float* bias) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const u32 i = mx_row_of(r, half), row = row0 + i;
-        const float s = row < end ? mx_score<BIAS>(d[r], scale, BIAS ? mx_bias(bias, row) : 0.f) : -kMxInf;
-        const float t = s - q_lse, p = expf(t);
-        // (p is 0 for rows that are out and for those far below, whose log p may be too large to multiply with)
-        s_c[i][lane % 32] = s == -kMxInf || p == 0.f ? 0.f : -p * (u_all + h * (t + q_entropy));
+    for (int p = 0; p < PIECES; ++p) {
+      u32 quad, word;
+      scales[p] = 0;
+      const bool in = place(p, &quad, &word);
+      const u32 byte = (col0 + 8 * word) / 2, block = (col0 + 8 * word) / kMxBlock;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32 row = row0 + 4 * quad + i;
+        codes[p][i] = 0;
+        // (a row that is out, or behind the last one, has zeros: also where it stands for NaN)
+        if (in && byte < row_bytes && row < end && !(BIAS && mx_bias(bias, row) == -kMxInf)) {
+          codes[p][i] = *reinterpret_cast<const u32*>(rows.codes + (u64)row * row_bytes + byte);
+          scales[p] |= (u32)rows.scales[(u64)row * blocks + block] << (8 * i);
+        }
       }
     }
-    for (u32 i = threadIdx.x; i < kMxTile * kMxGradColumns; i += kMxThreads) {
-      const u32 row = row0 + i / kMxGradColumns, col = col0 + i % kMxGradColumns;
-      // (a row that is out adds nothing, also where it stands for NaN)
-      const bool in = row < end && col < dim && !(BIAS && mx_bias(bias, row) == -kMxInf);
-      s_w[i / kMxGradColumns][i % kMxGradColumns] = in ? mx_value(rows, row, col, row_bytes, blocks) : 0.f;
-    }
-    __syncthreads();
-    const u32 q = threadIdx.x % 32, c0 = threadIdx.x / 32 * 8;
-    for (u32 i = 0; i < kMxTile; ++i)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sum[k] += s_c[i][q] * s_w[i][c0 + k];
   }
-  const u32 q = query0 + threadIdx.x % 32, c0 = col0 + threadIdx.x / 32 * 8;
-  if (q < queries.n)
-    for (int k = 0; k < 8; ++k)
-      if (c0 + k < dim) parts[((u64)part * queries.n + q) * dim + c0 + k] = sum[k];
+  // to: [COLUMNS / 32][2 steps][64 lanes][8 rows] of a tile
+  __device__ __forceinline__ void store(uint2* to) const {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      u32 quad, word;
+      if (!place(p, &quad, &word)) continue;
+      float s[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32 b = scales[p] >> (8 * i) & 255u;
+        s[i] = __uint_as_float(b ? b << 23 : 0x00400000u);
+      }
+      // rows 8 k + 4 half + i of a step (16 rows, k = 0, 1) are elements 4 k + i of lane half
+      const u32 step = quad / 4, k = quad / 2 % 2, half = quad % 2;
+      uint2* at = to + (((word / 4) * 2 + step) * kWave + half * 32 + word % 4 * 8) * 2 + k;
+#pragma unroll
+      for (int c = 0; c < 8; c += 2) {
+        u32 two[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          MxHalves2 v;
+          if (c == 0) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[p][i], s[i], 0);
+          else if (c == 2) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[p][i], s[i], 1);
+          else if (c == 4) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[p][i], s[i], 2);
+          else v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[p][i], s[i], 3);
+          two[i] = __builtin_bit_cast(u32, v);
+        }
+        at[2 * c] = make_uint2(__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u));
+        at[2 * c + 2] = make_uint2(__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u));
+      }
+    }
+  }
+};
+
+// What the exponents of a query are worked out with.
+struct MxGradUnit {
+  float unit;        // of a product (of a biased query: of a score), to a power of two
+  float off;         // the part of it that float32 does not hold, relative
+};
+
+// A workgroup: query_tiles (1, 2 or 4) x 32 queries, a part of the rows, of which each of 4 / query_tiles groups of waves
+// takes some tiles of every stage (and has a part of its own in `parts`), and COLUMNS columns.
+template <typename SHAPE, bool BIAS, bool ENTROPY, int COLUMNS>
+__global__ void __launch_bounds__(kMxGradWaves * kWave) HPS_MX_WAVES
+mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, MxGradUnit unit, const float* __restrict__ bias,
+            const float* __restrict__ lse, const float* __restrict__ entropy, const i32* __restrict__ given, const float* __restrict__ d_logp,
+            u32 n_given, const float* __restrict__ d_entropy, u32 query_tiles, u32 part_rows, float* __restrict__ parts) {
+  constexpr int BLOCKS = COLUMNS / 32;
+  constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;           // of 8 bytes, a tile's unpacked values
+  __shared__ uint2 s_rows[2][kMxStageTiles][kTileWords];
+  __shared__ float s_bias[kMxGradWaves][kMxTile];
+  const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const u32 splits = kMxGradWaves / query_tiles, split = wave / query_tiles;
+  const u32 query = (blockIdx.y * query_tiles + wave % query_tiles) * kMxTile + lane % 32, mine = min(query, queries.n - 1);
+  const u32 first = blockIdx.x * part_rows, end = min(rows.n - first, part_rows) + first, col0 = blockIdx.z * COLUMNS;
+
+  MxRow<SHAPE> q;
+  mx_load_row<SHAPE>(queries, mine, blocks, &q);
+  mx_clear_rest<SHAPE>(blocks, &q);
+  if (!BIAS && scale < 0.f) {
+#pragma unroll
+    for (int s = 0; s < SHAPE::STEPS; ++s) {
+      int4& c = q.codes[s];
+      c = make_int4(c.x ^ 0x88888888, c.y ^ 0x88888888, c.z ^ 0x88888888, c.w ^ 0x88888888);
+    }
+  }
+  // (-inf: all rows are out, and any number will do)
+  const float q_lse = lse[mine] == -kMxInf ? 0.f : lse[mine];
+  // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p
+  const float base = q_lse * kMxLog2e, rest = __fmaf_rn(q_lse, kMxLog2e, -base) + q_lse * 1.92596300e-8f;
+  const float correct = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base, -rest));
+  float a = 1.f, b = 0.f;
+  if (ENTROPY) {
+    float u = 0.f;
+    for (u32 g = half; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)mine * n_given + g, rows.n, bias);
+    u += __shfl_xor(u, 32, kWave);
+    const float h = d_entropy[mine];
+    a = -__fmaf_rn(h, entropy[mine], u);
+    b = -h * kMxLn2;
+  }
+  MxTile sum[BLOCKS];
+#pragma unroll
+  for (int k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();
+
+  MxUnpack<COLUMNS, BIAS> unpack;
+  unpack.load(rows, first + wave * kMxTile, end, col0, row_bytes, blocks, bias);
+  unpack.store(s_rows[0][wave]);
+  MxRow<SHAPE> next;
+  float next_bias = 0.f;
+  u32 next_row = min(first + split * kMxTile + lane % 32, rows.n - 1);
+  if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
+  if (BIAS) next_bias = mx_bias(bias, next_row);
+  __syncthreads();
+  u32 buffer = 0;
+  for (u32 stage0 = first; stage0 < end; stage0 += kMxStageRows, buffer ^= 1u) {
+    unpack.load(rows, stage0 + kMxStageRows + wave * kMxTile, end, col0, row_bytes, blocks, bias);
+    for (u32 tile = split; tile < kMxStageTiles; tile += splits) {
+      const u32 row0 = stage0 + tile * kMxTile;
+      if (row0 >= end) continue;
+      MxRow<SHAPE> r;
+      if (SHAPE::AHEAD) r = next;
+      else mx_load_row<SHAPE>(rows, min(row0 + lane % 32, rows.n - 1), blocks, &r);
+      const float my_bias = row0 + lane % 32 < end ? next_bias : -kMxInf;
+      const u32 ahead = tile + splits < kMxStageTiles ? row0 + splits * kMxTile : stage0 + kMxStageRows + split * kMxTile;
+      next_row = min(ahead + lane % 32, rows.n - 1);
+      if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
+      float x_bias[16];
+      if (BIAS) {
+        next_bias = mx_bias(bias, next_row);
+        if (my_bias == -kMxInf) {
+#pragma unroll
+          for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r.scales[w] = 0;
+        }
+        __builtin_amdgcn_wave_barrier();
+        s_bias[wave][lane % 32] = my_bias;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 v = *reinterpret_cast<const float4*>(&s_bias[wave][8 * g + 4 * half]);
+          x_bias[4 * g] = v.x; x_bias[4 * g + 1] = v.y; x_bias[4 * g + 2] = v.z; x_bias[4 * g + 3] = v.w;
+        }
+      }
+      const MxTile d = mx_products<SHAPE>(r, q, blocks);
+      u32 piece[3][8];            // pairs of rows, first / second / last eight bits of c
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        u32 bits[2][3];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float t = BIAS ? (__fmaf_rn(d[i + k], scale, x_bias[i + k]) - q_lse) * unit.unit : __fmaf_rn(d[i + k], unit.unit, -base);
+          float c = exp2_fast(t);
+          // (log p of a row far below, or out, is not multiplied with: its p is 0)
+          if (ENTROPY) c *= __fmaf_rn(b, BIAS ? fmaxf(t, -200.f) : t, a);
+          float left = c;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) {
+            bits[k][j] = __float_as_uint(left);
+            left -= __uint_as_float(bits[k][j] & 0xFFFF0000u);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j) piece[j][i / 2] = __builtin_amdgcn_perm(bits[1][j], bits[0][j], 0x07060302u);
+      }
+#pragma unroll
+      for (int step = 0; step < 2; ++step) {
+        MxHalves8 value[BLOCKS];
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k)
+          value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][((k * 2 + step) * kWave + lane) * 2]);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+          const uint4 w = make_uint4(piece[j][4 * step], piece[j][4 * step + 1], piece[j][4 * step + 2], piece[j][4 * step + 3]);
+#pragma unroll
+          for (int k = 0; k < BLOCKS; ++k)
+            sum[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[k], 0, 0, 0);
+        }
+      }
+    }
+    unpack.store(s_rows[buffer ^ 1u][wave]);
+    __syncthreads();
+  }
+  if (query >= queries.n) return;
+  float* to = parts + ((u64)(blockIdx.x * splits + split) * queries.n + query) * dim;
+#pragma unroll
+  for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const u32 col = col0 + k * 32 + 8 * g + 4 * half;
+      if (col < dim)
+        *reinterpret_cast<float4*>(to + col) = make_float4(sum[k][4 * g] * correct, sum[k][4 * g + 1] * correct, sum[k][4 * g + 2] * correct,
+                                                           sum[k][4 * g + 3] * correct);
+    }
 }
 
-template <bool BIAS>
-__global__ void __launch_bounds__(kMxThreads)
+// The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.
+constexpr u32 kMxEndWaves = 16;
+template <bool BIAS, bool ENTROPY>
+__global__ void __launch_bounds__(kMxEndWaves * kWave)
 mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, float scale, const float* __restrict__ bias,
                 const i32* __restrict__ given, const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ parts,
                 u32 n_parts, float* __restrict__ out) {
-  const u64 total = (u64)n_queries * dim;
-  for (u64 i = (u64)blockIdx.x * kMxThreads + threadIdx.x; i < total; i += (u64)gridDim.x * kMxThreads) {
+  __shared__ float s_sum[kMxEndWaves][kWave], s_given[kMxEndWaves][kWave], s_u[kMxEndWaves][kWave];
+  const u32 lane = lane_id(), wave = threadIdx.x / kWave;
+  const u64 total = (u64)n_queries * dim, i = (u64)blockIdx.x * kWave + lane;
+  if (i < total) {
     const u32 query = (u32)(i / dim), col = (u32)(i - (u64)query * dim);
-    float sum = 0.f;
-    for (u32 p = 0; p < n_parts; ++p) sum += parts[p * total + i];
-    for (u32 g = 0; g < n_given; ++g) {
+    float sum = 0.f, of_given = 0.f, u_all = 0.f;
+#pragma unroll 8
+    for (u32 p = wave; p < n_parts; p += kMxEndWaves) sum += parts[p * total + i];
+    for (u32 g = wave; g < n_given; g += kMxEndWaves) {
       const u64 at = (u64)query * n_given + g;
       const float u = mx_upstream<BIAS>(given, d_logp, at, rows.n, bias);
-      if (u != 0.f) sum += u * mx_value(rows, (u32)given[at], col, row_bytes, blocks);
+      u_all += u;
+      if (u != 0.f) of_given += u * mx_value(rows, (u32)given[at], col, row_bytes, blocks);
     }
-    out[i] = scale * sum;
+    s_sum[wave][lane] = sum;
+    s_given[wave][lane] = of_given;
+    s_u[wave][lane] = u_all;
+  }
+  __syncthreads();
+  if (wave == 0 && i < total) {
+    float sum = 0.f, of_given = 0.f, u_all = 0.f;
+#pragma unroll
+    for (u32 w = 0; w < kMxEndWaves; ++w) {
+      sum += s_sum[w][lane];
+      of_given += s_given[w][lane];
+      u_all += s_u[w][lane];
+    }
+    out[i] = scale * ((ENTROPY ? sum : -u_all * sum) + of_given);
   }
 }
 

@@ -23,6 +23,7 @@ uint64_t mx_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 // a part share an XCD and with it the L2 that holds its rows.
 constexpr uint64_t kMxWaves = 4096;
 constexpr uint64_t kMxFewQueries = 256;
+constexpr uint64_t kMxGradGroups = 1024;           // workgroups of mx_gradient
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
 };
@@ -210,10 +211,28 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
 }
 
+// The gradient's division: workgroups of 128 queries (fewer queries: the waves share the rows instead) and a part of the rows each.
+struct MxGradSplit {
+  uint64_t query_tiles, query_groups, columns, column_groups, part_rows, parts, sums;
+};
+static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
+  MxGradSplit s;
+  const uint64_t tiles = mx_ceil(n_queries, kMxTile);
+  s.query_tiles = tiles > 2 ? 4 : tiles;
+  s.query_groups = mx_ceil(tiles, s.query_tiles);
+  s.columns = dim <= 32 ? 32 : dim <= 64 ? 64 : 128;
+  s.column_groups = mx_ceil(dim, s.columns);
+  const uint64_t wanted = mx_ceil(std::max<uint64_t>(1, kMxGradGroups / (s.query_groups * s.column_groups)), kXcds) * kXcds;
+  s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), kMxStageRows) * kMxStageRows;
+  s.parts = mx_ceil(n_rows, s.part_rows);
+  s.sums = s.parts * (kMxGradWaves / s.query_tiles);
+  return s;
+}
+
 size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
   if (!mx_sizes_ok(n_queries, n_rows, dim)) return 0;
   if (n_queries == 0 || n_rows == 0) return kAlign;
-  return align_up(mx_split(n_queries, n_rows, dim, 0, 1, kMxWaves / 4).parts * n_queries * dim * sizeof(float));
+  return align_up(mx_grad_split(n_queries, n_rows, dim).sums * n_queries * dim * sizeof(float));
 }
 
 hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
@@ -232,23 +251,35 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
     return HPS_EINVAL;
   if (workspace_bytes < hps_mx4_logprobs_backward_bytes(m, rows->n, dim)) return HPS_ENOMEM;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  MxSplit p = {};
+  MxGradSplit p = {};
   float* parts = static_cast<float*>(d_workspace);
   const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
-  if (rows->n) {
-    p = mx_split(m, rows->n, dim, 0, 1, kMxWaves / 4);
-    mx_by_width(dim, [&](auto width) {
-      mx_by_flag(d_bias != nullptr, [&](auto biased) {
-        mx_gradient<decltype(width)::value, decltype(biased)::value>
-            <<<dim3((unsigned)p.parts, (unsigned)p.query_tiles, (unsigned)mx_ceil(dim, kMxGradColumns)), kMxThreads, 0, s>>>(
-                mx_held(queries), mx_held(rows), dim, blocks, row_bytes, scale, d_bias, d_lse, d_entropy, d_given, d_dlogp, n_given,
-                d_dentropy, (u32)p.part_rows, parts);
-      });
-    });
-  }
   mx_by_flag(d_bias != nullptr, [&](auto biased) {
-    mx_gradient_end<decltype(biased)::value><<<grid_for(m * dim, kMxThreads, 1u << 16), kMxThreads, 0, s>>>(
-        mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, d_given, d_dlogp, n_given, parts, (u32)p.parts, d_dqueries);
+    mx_by_flag(d_dentropy != nullptr, [&](auto with_entropy) {
+      constexpr bool B = decltype(biased)::value, E = decltype(with_entropy)::value;
+      if (rows->n) {
+        p = mx_grad_split(m, rows->n, dim);
+        const double exact = B ? 1.4426950408889634 : std::fabs((double)scale) * 1.4426950408889634;
+        const float held = B ? kMxLog2e : std::fabs(scale) * kMxLog2e;
+        const MxGradUnit unit = {held, held > 0.f ? (float)(exact / held - 1.0) : 0.f};
+        const dim3 grid((unsigned)p.parts, (unsigned)p.query_groups, (unsigned)p.column_groups);
+        mx_by_shape(dim, [&](auto shape) {
+          typedef decltype(shape) Shape;
+          constexpr int COLUMNS = Shape::WIDTH < 16 ? 32 : Shape::STEPS == 1 ? 64 : 128;
+#define HPS_MX_GRADIENT(COLUMNS)                                                                                             \
+  mx_gradient<Shape, B, E, COLUMNS><<<grid, kMxGradWaves * kWave, 0, s>>>(                                                   \
+      mx_held(queries), mx_held(rows), dim, blocks, row_bytes, scale, unit, d_bias, d_lse, d_entropy, d_given, d_dlogp,      \
+      n_given, d_dentropy, (u32)p.query_tiles, (u32)p.part_rows, parts)
+          if constexpr (Shape::WIDTH == 16 && Shape::STEPS == 1) {
+            if (p.columns == 32) { HPS_MX_GRADIENT(32); return; }
+          }
+          HPS_MX_GRADIENT(COLUMNS);
+#undef HPS_MX_GRADIENT
+        });
+      }
+      mx_gradient_end<B, E><<<(unsigned)mx_ceil(m * dim, kWave), kMxEndWaves * kWave, 0, s>>>(
+          mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, d_given, d_dlogp, n_given, parts, (u32)p.sums, d_dqueries);
+    });
   });
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
 }

@@ -125,14 +125,16 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
   }
   MxRow<SHAPE> next;
   float next_bias = 0.f;
-  mx_load_row<SHAPE>(rows, min(first + lane % 32, rows.n - 1), blocks, &next);
+  if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, min(first + lane % 32, rows.n - 1), blocks, &next);
   if (BIAS) next_bias = mx_bias(bias, min(first + lane % 32, rows.n - 1));
   u32 in_group = 0;
   for (u32 row0 = first; row0 < end; row0 += kMxTile) {
-    MxRow<SHAPE> r = next;
+    MxRow<SHAPE> r;
+    if (SHAPE::AHEAD) r = next;
+    else mx_load_row<SHAPE>(rows, min(row0 + lane % 32, rows.n - 1), blocks, &r);
     const float my_bias = row0 + lane % 32 < end ? next_bias : -kMxInf;
     const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
-    mx_load_row<SHAPE>(rows, ahead, blocks, &next);
+    if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, ahead, blocks, &next);
     float b[16] = {};
     if (BIAS) {
       next_bias = mx_bias(bias, ahead);
