@@ -6,6 +6,8 @@ namespace {
 constexpr uint64_t kMxMaxQueries = 1ull << 20;
 constexpr uint64_t kMxMaxRows = (1ull << 31) - 1;
 constexpr uint64_t kMxMaxBlocks = 1ull << 30;      // workgroups a launch may have
+constexpr uint64_t kMxMaxScores = 1ull << 40;      // scores of a call, more than a GPU has room for
+constexpr uint64_t kMxScoreGroups = 2048;          // workgroups of mx_scores that fill the GPU
 
 bool mx_dim_ok(uint32_t dim) { return dim >= 4 && dim <= 1024 && dim % 4 == 0; }
 bool mx_aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -133,17 +135,22 @@ hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows,
   if (queries->n == 0 || rows->n == 0) return HPS_OK;
   const bool bf16 = type == HPS_VALUES_BF16;
   if (!d_out || !mx_aligned(d_out, bf16 ? 2 : 4) || !mx_aligned(d_bias, 4)) return HPS_EINVAL;
-  const uint64_t row_tiles = mx_ceil(rows->n, kMxTile * (kMxThreads / kWave)), blocks = row_tiles * mx_ceil(queries->n, kMxTile);
-  if (blocks > kMxMaxBlocks) return HPS_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  mx_by_width(dim, [&](auto width) {
+  hps_status rc = HPS_OK;
+  mx_by_shape(dim, [&](auto shape) {
+    typedef decltype(shape) Shape;
+    const uint64_t row_groups = mx_ceil(rows->n, mx_score_tiles<Shape>() * kMxTile * (kMxThreads / kWave)), tiles = mx_ceil(queries->n, kMxTile);
+    // a part of the queries for every workgroup, as long as that leaves enough of them
+    const uint64_t part_tiles = mx_ceil(tiles, std::max<uint64_t>(1, kMxScoreGroups / row_groups)), parts = mx_ceil(tiles, part_tiles);
+    if (row_groups * parts > kMxMaxBlocks || rows->n * queries->n > kMxMaxScores) { rc = HPS_EINVAL; return; }
     mx_by_flag(d_bias != nullptr, [&](auto biased) {
       mx_by_flag(bf16, [&](auto narrow) {
-        mx_scores<decltype(width)::value, decltype(biased)::value, decltype(narrow)::value><<<(unsigned)blocks, kMxThreads, 0, s>>>(
-            mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, d_out, stride, (u32)row_tiles);
+        mx_scores<Shape, decltype(biased)::value, decltype(narrow)::value><<<(unsigned)(row_groups * parts), kMxThreads, 0, s>>>(
+            mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, d_out, stride, (u32)row_groups, (u32)parts, (u32)part_tiles);
       });
     });
   });
+  if (rc != HPS_OK) return rc;
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
 }
 

@@ -1,31 +1,89 @@
 // All scores of queries against rows (include/hps_mx4.h: hps_mx4_scores).
 //
-// One wave computes 32 queries x 32 rows; lanes lie along the rows, so that each store of a register writes
-// 32 neighbouring scores of a query.
+// What bounds it is writing the scores: 4 (or 2) bytes for 2 dim operations, of which the matrix units do some thousand in
+// the time that a byte takes.  So the lanes lie along the rows, and a wave's tiles are dealt out so that a lane has
+// neighbouring rows of a query (tile t holds rows RT j + t): a store writes RT neighbouring scores a lane, whole lines a wave.
+// A wave holds RT x 32 rows and goes through the query tiles of its part; the rows' operands stay in
+// registers, the queries', which all waves share, come out of the caches.
 #pragma once
 
 #include "mx4.hpp"
 
 namespace hps {
 
-template <int WIDTH, bool BIAS, bool BF16>
-__global__ void __launch_bounds__(kMxThreads)
-mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, void* __restrict__ out, u64 stride,
-          u32 row_tiles) {
-  const u32 lane = lane_id(), half = lane / 32, wave = threadIdx.x / kWave;
-  const u32 row_tile = blockIdx.x % row_tiles, query_tile = blockIdx.x / row_tiles;
-  const u32 row = (row_tile * (kMxThreads / kWave) + wave) * kMxTile + lane % 32, query0 = query_tile * kMxTile;
-  if (row - lane % 32 >= rows.n) return;
-  const MxTile d = mx_products_once<WIDTH>(queries, min(query0 + lane % 32, queries.n - 1), rows, min(row, rows.n - 1), blocks);
-  if (row >= rows.n) return;
-  const float b = BIAS ? mx_bias(bias, row) : 0.f;
+// Stores RT neighbouring scores of a query, of which the first `n` are there.  (The GPU stores words of any alignment.)
+template <int RT, bool BF16>
+__device__ __forceinline__ void mx_store_scores(void* out, u64 at, const float* s, u32 n) {
+  if (BF16) {
+    typedef u32 Pairs __attribute__((ext_vector_type(RT / 2), aligned(2)));
+    uint16_t* to = static_cast<uint16_t*>(out) + at;
+    if (n == RT) {
+      Pairs v;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const u32 q = query0 + mx_row_of(r, half);
-    if (q >= queries.n) continue;
-    const float s = mx_score<BIAS>(d[r], scale, b);
-    if (BF16) static_cast<uint16_t*>(out)[q * stride + row] = (uint16_t)bf16_nearest(s);
-    else static_cast<float*>(out)[q * stride + row] = s;
+      for (int t = 0; t < RT / 2; ++t) v[t] = bf16_nearest(s[2 * t]) | bf16_nearest(s[2 * t + 1]) << 16;
+      __builtin_nontemporal_store(v, reinterpret_cast<Pairs*>(to));
+      return;
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+      if (t < (int)n) to[t] = (uint16_t)bf16_nearest(s[t]);
+    return;
+  }
+  typedef float Floats __attribute__((ext_vector_type(RT), aligned(4)));
+  float* to = static_cast<float*>(out) + at;
+  if (n == RT) {
+    Floats v;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) v[t] = s[t];
+    __builtin_nontemporal_store(v, reinterpret_cast<Floats*>(to));
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+    if (t < (int)n) to[t] = s[t];
+}
+
+// Tiles of rows a wave holds.
+template <typename SHAPE>
+constexpr int mx_score_tiles() { return SHAPE::STEPS <= 4 ? 4 : 2; }
+
+template <typename SHAPE, bool BIAS, bool BF16>
+__global__ void __launch_bounds__(kMxThreads) HPS_MX_WAVES
+mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, void* __restrict__ out, u64 stride,
+          u32 row_groups, u32 query_parts, u32 part_tiles) {
+  constexpr int RT = mx_score_tiles<SHAPE>();
+  const u32 lane = lane_id(), half = lane / 32, wave = threadIdx.x / kWave;
+  // neighbouring pieces of work, which share rows, to one XCD
+  const u32 piece = xcd_piece(blockIdx.x, gridDim.x), row_group = piece / query_parts, query_part = piece - row_group * query_parts;
+  const u32 row0 = (row_group * (kMxThreads / kWave) + wave) * (RT * kMxTile), row = row0 + lane % 32 * RT;
+  if (row0 >= rows.n) return;
+  MxRow<SHAPE> r[RT];
+  float b[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const u32 at = min(row + t, rows.n - 1);
+    mx_load_row<SHAPE>(rows, at, blocks, &r[t]);
+    b[t] = BIAS ? mx_bias(bias, at) : 0.f;
+  }
+  const u32 left = row < rows.n ? min(rows.n - row, (u32)RT) : 0;
+  const u32 tiles = (queries.n + kMxTile - 1) / kMxTile, last = min(query_part * part_tiles + part_tiles, tiles);
+  for (u32 tile = query_part * part_tiles; tile < last; ++tile) {
+    const u32 query0 = tile * kMxTile;
+    MxRow<SHAPE> q;
+    mx_load_row<SHAPE>(queries, min(query0 + lane % 32, queries.n - 1), blocks, &q);
+    mx_clear_rest<SHAPE>(blocks, &q);
+    MxTile d[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) d[t] = mx_products<SHAPE>(q, r[t], blocks);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const u32 query = query0 + mx_row_of(i, half);
+      if (query >= queries.n) continue;
+      float s[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) s[t] = mx_score<BIAS>(d[t][i], scale, b[t]);
+      mx_store_scores<RT, BF16>(out, query * stride + row, s, left);
+    }
   }
 }
 
