@@ -15,7 +15,7 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple, Optional
 
-from .binding import EINVAL, HpsError, Mx4Operand, _check, _ptr, lib
+from .binding import EINVAL, OK, HpsError, Mx4Operand, _ptr, lib
 
 MX4_MAX_TOP = 64
 
@@ -29,29 +29,30 @@ def _row_shape(dim: int):
 
 class Mx4Rows:
     """Rows in the 4-bit form: codes uint8 [n, hps_mx4_row_bytes(dim)], scales uint8 [n, hps_mx4_row_scales(dim)]."""
-    __slots__ = ("codes", "scales", "dim", "n")
+    __slots__ = ("codes", "scales", "dim", "n", "device")
 
     def __init__(self, codes, scales, dim: int):
         import torch
         n, shape = codes.shape[0], _row_shape(dim)
-        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.shape != (n, shape[0]) or scales.shape != (n, shape[1]):
+        if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or codes.shape != (n, shape[0]) or scales.shape != (n, shape[1]):
             raise ValueError("rows of dim %d: codes must be uint8 [n, %d] and scales uint8 [n, %d]" % ((dim,) + shape))
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("codes and scales must be contiguous")
-        if not codes.is_cuda or codes.device != scales.device:
+        device = codes.device
+        if device.type != "cuda" or scales.device != device:
             raise ValueError("codes and scales must be on one GPU")
-        self.codes, self.scales, self.dim, self.n = codes, scales, dim, n
+        self.codes, self.scales, self.dim, self.n, self.device = codes, scales, dim, n, device
 
     @classmethod
     def empty(cls, n: int, dim: int, device) -> "Mx4Rows":
+        """Rows to be written."""
         import torch
         shape = _row_shape(dim)
-        return cls(torch.empty((n, shape[0]), dtype=torch.uint8, device=device),
-                   torch.empty((n, shape[1]), dtype=torch.uint8, device=device), dim)
-
-    @property
-    def device(self):
-        return self.codes.device
+        rows = cls.__new__(cls)
+        rows.codes = torch.empty((n, shape[0]), dtype=torch.uint8, device=device)
+        rows.scales = torch.empty((n, shape[1]), dtype=torch.uint8, device=device)
+        rows.dim, rows.n, rows.device = dim, n, rows.codes.device
+        return rows
 
     def __getitem__(self, part: slice) -> "Mx4Rows":
         """A range of the rows, in place."""
@@ -59,37 +60,28 @@ class Mx4Rows:
             raise TypeError("rows are taken by ranges")
         return Mx4Rows(self.codes[part], self.scales[part], self.dim)
 
-    def _operand(self) -> Mx4Operand:
-        return Mx4Operand(self.codes.data_ptr(), self.scales.data_ptr(), self.n)
+    def _operand(self):
+        return ctypes.byref(Mx4Operand(self.codes.data_ptr(), self.scales.data_ptr(), self.n))
 
     def dequantize(self):
         """The values that the rows stand for, float32 [n, dim]."""
         import torch
         out = torch.empty((self.n, self.dim), dtype=torch.float32, device=self.device)
-        with _On(self.device) as stream:
-            _check(lib().hps_mx4_dequantize(ctypes.byref(self._operand()), self.dim, _ptr(out), stream), "hps_mx4_dequantize")
+        _call("hps_mx4_dequantize", self.device, self._operand(), self.dim, out.data_ptr())
         return out
 
 
-class _On:
-    """Makes a tensor's GPU the current one for a call; gives the current stream there."""
-    __slots__ = ("device", "before")
-
-    def __init__(self, device):
-        self.device = device.index
-
-    def __enter__(self):
-        from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
-        self.before = _cuda_getDevice()
-        if self.before != self.device:
-            import torch
-            torch.cuda.set_device(self.device)
-        return _cuda_getCurrentRawStream(self.device)
-
-    def __exit__(self, *_):
-        if self.before != self.device:
-            import torch
-            torch.cuda.set_device(self.before)
+def _call(name: str, device, *args) -> None:
+    """Calls an entry point with `device` the current GPU, on its current stream."""
+    import torch
+    fn, index = getattr(lib(), name), device.index
+    if torch._C._cuda_getDevice() == index:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status != OK:
+        raise HpsError(status, name)
 
 
 class LogProbs(NamedTuple):
@@ -102,57 +94,66 @@ class LogProbs(NamedTuple):
 
 
 def _array(t, name: str, dtype, shape, device):
-    """A contiguous tensor of this type, shape and GPU (None stays None)."""
+    """Address of a contiguous tensor of this type, shape and GPU (None stays None)."""
     if t is None:
-        return
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, shape, device))
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
+    return t.data_ptr()
 
 
-def _pair(queries: Mx4Rows, rows: Mx4Rows, bias):
+def _pair(queries: Mx4Rows, rows: Mx4Rows):
     if queries.dim != rows.dim:
         raise ValueError("queries of dim %d and rows of dim %d" % (queries.dim, rows.dim))
     if queries.device != rows.device:
         raise ValueError("queries and rows must be on one GPU")
-    if bias is not None:
-        import torch
-        _array(bias, "bias", torch.float32, (rows.n,), rows.device)
+
+
+def _given(given, m: int, device):
+    """(address, how many a query)"""
+    if given is None:
+        return None, 0
+    import torch
+    if given.dim() != 2:
+        raise ValueError("given must be [queries, g]")
+    g = given.shape[1]
+    return _array(given, "given", torch.int32, (m, g), device), g
 
 
 def mx4_quantize(x, values: bool = False):
     """Mx4Rows of x [n, dim] (float32 or bfloat16; its rows may lie apart); with values=True also the values they stand
     for, float32 [n, dim]."""
     import torch
-    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda:
+    dtype = x.dtype
+    if x.dim() != 2 or (dtype is not torch.float32 and dtype is not torch.bfloat16) or not x.is_cuda:
         raise ValueError("x must be a float32 or bfloat16 CUDA tensor [n, dim]")
     n, dim = x.shape
-    if x.stride(1) != 1 and n and dim > 1:
+    apart, step = x.stride()
+    if step != 1 and n and dim > 1:
         raise ValueError("the values of a row must lie next to each other")
-    stride = x.stride(0) if n > 1 else dim
     rows = Mx4Rows.empty(n, dim, x.device)
-    rounded = torch.empty((n, dim), dtype=torch.float32, device=x.device) if values else None
-    with _On(x.device) as stream:
-        _check(lib().hps_mx4_quantize(_ptr(x), 1 if x.dtype == torch.bfloat16 else 0, n, dim, stride, _ptr(rows.codes),
-                                      _ptr(rows.scales), _ptr(rounded), stream), "hps_mx4_quantize")
+    rounded = torch.empty((n, dim), dtype=torch.float32, device=rows.device) if values else None
+    _call("hps_mx4_quantize", rows.device, x.data_ptr(), 0 if dtype is torch.float32 else 1, n, dim, apart if n > 1 else dim,
+          rows.codes.data_ptr(), rows.scales.data_ptr(), rounded.data_ptr() if values else None)
     return (rows, rounded) if values else rows
 
 
 def mx4_scores(queries: Mx4Rows, rows: Mx4Rows, scale: float = 1.0, bias=None, dtype=None, out=None):
     """scale * <query, row> + bias of every query and row: [queries, rows], float32 or bfloat16 (`out`: written there)."""
     import torch
-    _pair(queries, rows, bias)
+    _pair(queries, rows)
+    m, n, device = queries.n, rows.n, rows.device
     if out is None:
-        out = torch.empty((queries.n, rows.n), dtype=dtype or torch.float32, device=rows.device)
+        out = torch.empty((m, n), dtype=dtype or torch.float32, device=device)
     elif dtype is not None and dtype != out.dtype:
         raise ValueError("out is not of the type asked for")
-    if out.dtype not in (torch.float32, torch.bfloat16) or tuple(out.shape) != (queries.n, rows.n) or out.device != rows.device:
+    if (out.dtype is not torch.float32 and out.dtype is not torch.bfloat16) or out.shape != (m, n) or out.device != device:
         raise ValueError("the scores are float32 or bfloat16 [queries, rows], on the rows' GPU")
-    if out.stride(1) != 1 and rows.n > 1 and queries.n:
+    apart, step = out.stride()
+    if step != 1 and n > 1 and m:
         raise ValueError("the scores of a query must lie next to each other")
-    stride = out.stride(0) if queries.n > 1 else rows.n
-    with _On(rows.device) as stream:
-        _check(lib().hps_mx4_scores(ctypes.byref(queries._operand()), ctypes.byref(rows._operand()), rows.dim, scale, _ptr(bias),
-                                    _ptr(out), 1 if out.dtype == torch.bfloat16 else 0, stride, stream), "hps_mx4_scores")
+    _call("hps_mx4_scores", device, queries._operand(), rows._operand(), rows.dim, scale, _array(bias, "bias", torch.float32, (n,), device),
+          out.data_ptr(), 0 if out.dtype is torch.float32 else 1, apart if m > 1 else n)
     return out
 
 
@@ -160,25 +161,19 @@ def mx4_logprobs(queries: Mx4Rows, rows: Mx4Rows, given=None, top: int = 0, scal
     """Log-sum-exp and entropy of each query's scores; log probabilities of the given rows (int32 [queries, g]); the `top`
     best rows (int32 numbers and log probabilities, best first)."""
     import torch
-    _pair(queries, rows, bias)
-    m, device, g = queries.n, rows.device, 0
+    _pair(queries, rows)
+    m, n, dim, device = queries.n, rows.n, rows.dim, rows.device
     if top < 0 or top > MX4_MAX_TOP:
         raise HpsError(EINVAL, "top %d" % top)
-    if given is not None:
-        if given.dim() != 2:
-            raise ValueError("given must be [queries, g]")
-        g = given.shape[1]
-        _array(given, "given", torch.int32, (m, g), device)
-    lse, entropy = torch.empty((2, m), dtype=torch.float32, device=device)
+    asked, g = _given(given, m, device)
+    lse, entropy = torch.empty(m, dtype=torch.float32, device=device), torch.empty(m, dtype=torch.float32, device=device)
     logp = torch.empty((m, g), dtype=torch.float32, device=device) if given is not None else None
     index = torch.empty((m, top), dtype=torch.int32, device=device) if top else None
     best = torch.empty((m, top), dtype=torch.float32, device=device) if top else None
-    size = lib().hps_mx4_logprobs_bytes(m, rows.n, rows.dim, top)
+    size = lib().hps_mx4_logprobs_bytes(m, n, dim, top)
     space = torch.empty(size, dtype=torch.uint8, device=device)
-    with _On(device) as stream:
-        _check(lib().hps_mx4_logprobs(ctypes.byref(queries._operand()), ctypes.byref(rows._operand()), rows.dim, scale, _ptr(bias),
-                                      _ptr(given), g, top, _ptr(lse), _ptr(entropy), _ptr(logp), _ptr(index), _ptr(best), _ptr(space),
-                                      size, stream), "hps_mx4_logprobs")
+    _call("hps_mx4_logprobs", device, queries._operand(), rows._operand(), dim, scale, _array(bias, "bias", torch.float32, (n,), device), asked,
+          g, top, lse.data_ptr(), entropy.data_ptr(), _ptr(logp), _ptr(index), _ptr(best), space.data_ptr(), size)
     return LogProbs(lse, entropy, logp, index, best)
 
 
@@ -187,25 +182,21 @@ def mx4_logprobs_backward(queries: Mx4Rows, rows: Mx4Rows, given, d_logp, lse, e
     """The gradient of sum(d_logp * logp) + sum(d_entropy * entropy) with respect to the values that the queries stand
     for, float32 [queries, dim].  lse, entropy: of mx4_logprobs, for the same arguments."""
     import torch
-    _pair(queries, rows, bias)
-    m, device, g = queries.n, rows.device, 0
+    _pair(queries, rows)
+    m, n, dim, device = queries.n, rows.n, rows.dim, rows.device
     if (given is None) != (d_logp is None):
         raise ValueError("given rows and their gradients come together")
-    if given is not None:
-        if given.dim() != 2:
-            raise ValueError("given must be [queries, g]")
-        g = given.shape[1]
-        _array(given, "given", torch.int32, (m, g), device)
-        _array(d_logp, "d_logp", torch.float32, (m, g), device)
+    asked, g = _given(given, m, device)
     if d_entropy is not None and entropy is None:
         raise ValueError("a gradient of the entropy needs the entropy")
-    for name, t in (("lse", lse), ("entropy", entropy), ("d_entropy", d_entropy)):
-        _array(t, name, torch.float32, (m,), device)
-    out = torch.empty((m, rows.dim), dtype=torch.float32, device=device)
-    size = lib().hps_mx4_logprobs_backward_bytes(m, rows.n, rows.dim)
+    if lse is None:
+        raise ValueError("lse of mx4_logprobs is needed")
+    args = (_array(bias, "bias", torch.float32, (n,), device), _array(lse, "lse", torch.float32, (m,), device),
+            _array(entropy, "entropy", torch.float32, (m,), device), asked, _array(d_logp, "d_logp", torch.float32, (m, g), device), g,
+            _array(d_entropy, "d_entropy", torch.float32, (m,), device))
+    out = torch.empty((m, dim), dtype=torch.float32, device=device)
+    size = lib().hps_mx4_logprobs_backward_bytes(m, n, dim)
     space = torch.empty(size, dtype=torch.uint8, device=device)
-    with _On(device) as stream:
-        _check(lib().hps_mx4_logprobs_backward(ctypes.byref(queries._operand()), ctypes.byref(rows._operand()), rows.dim, scale,
-                                               _ptr(bias), _ptr(lse), _ptr(entropy), _ptr(given), _ptr(d_logp), g, _ptr(d_entropy),
-                                               _ptr(out), _ptr(space), size, stream), "hps_mx4_logprobs_backward")
+    _call("hps_mx4_logprobs_backward", device, queries._operand(), rows._operand(), dim, scale, *args, out.data_ptr(), space.data_ptr(),
+          size)
     return out
