@@ -31,49 +31,51 @@ __device__ __forceinline__ float mx_value(const MxHeld& m, u32 row, u32 col, u32
   return mx_decode(codes, m.scales[(u64)row * blocks + col / kMxBlock]).v[0];
 }
 
-// The upstream gradient of a given row, 0 where it has no part in it.
+// The upstream gradient of a given row, 0 where it has no part in it.  (Loads first: several of these are in flight.)
 template <bool BIAS>
 __device__ __forceinline__ float mx_upstream(const i32* given, const float* d_logp, u64 at, u32 n_rows, const float* bias) {
-  const i32 g = given[at];
-  const float u = d_logp[at];
-  if (g < 0 || (u32)g >= n_rows) return 0.f;
-  if (BIAS && mx_bias(bias, (u32)g) == -kMxInf) return 0.f;
-  return u;
+  const u32 g = (u32)given[at];                 // (a negative number is beyond the last row)
+  const float u = d_logp[at], b = BIAS ? mx_bias(bias, min(g, n_rows - 1)) : 0.f;
+  return g >= n_rows || (BIAS && b == -kMxInf) ? 0.f : u;
+}
+
+// Where a tile's unpacked values lie, in units of 16 bytes (eight rows of a column): what lane `at` of a step of a block of 32
+// columns reads.  The last three bits are mixed with those by which the lanes that write at one time differ, as these
+// would otherwise all meet the same few banks.
+__device__ __forceinline__ u32 mx_unit(u32 block, u32 step, u32 at) {
+  return (block * 2 + step) * kWave + (at ^ (at >> 4 & 1u) ^ (at >> 5 & 1u) << 1 ^ step << 2);
 }
 
 // Unpacking: a lane takes eight columns of four neighbouring rows, 8 x COLUMNS / 8 such pieces a tile.
 template <int COLUMNS, bool BIAS>
 struct MxUnpack {
   static constexpr int PIECES = (COLUMNS + kWave / 8 * 8 - 1) / (kWave / 8 * 8);       // a lane's pieces of a tile
-  u32 codes[PIECES][4];
-  u32 scales[PIECES];                                                                    // a byte each
+  u32 codes[PIECES][4], scales[PIECES][4];
+  float bias[PIECES][4];
   static __device__ __forceinline__ bool place(int piece, u32* quad, u32* word) {
     const u32 at = piece * kWave + lane_id();
     *quad = at % 8;
     *word = at / 8;
     return *word < COLUMNS / 8;
   }
-  __device__ __forceinline__ void load(const MxHeld& rows, u32 row0, u32 end, u32 col0, u32 row_bytes, u32 blocks, const float* bias) {
+  __device__ __forceinline__ void load(const MxHeld& rows, u32 row0, u32 col0, u32 row_bytes, u32 blocks, const float* of_rows) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       u32 quad, word;
-      scales[p] = 0;
-      const bool in = place(p, &quad, &word);
-      const u32 byte = (col0 + 8 * word) / 2, block = (col0 + 8 * word) / kMxBlock;
+      place(p, &quad, &word);
+      // (what is not there is read elsewhere, and left out when it is stored)
+      const u32 byte = min((col0 + 8 * word) / 2, row_bytes - 4), block = min((col0 + 8 * word) / kMxBlock, blocks - 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32 row = row0 + 4 * quad + i;
-        codes[p][i] = 0;
-        // (a row that is out, or behind the last one, has zeros: also where it stands for NaN)
-        if (in && byte < row_bytes && row < end && !(BIAS && mx_bias(bias, row) == -kMxInf)) {
-          codes[p][i] = *reinterpret_cast<const u32*>(rows.codes + (u64)row * row_bytes + byte);
-          scales[p] |= (u32)rows.scales[(u64)row * blocks + block] << (8 * i);
-        }
+        const u32 row = min(row0 + 4 * quad + i, rows.n - 1);
+        codes[p][i] = *reinterpret_cast<const u32*>(rows.codes + (u64)row * row_bytes + byte);
+        scales[p][i] = rows.scales[(u64)row * blocks + block];
+        if (BIAS) bias[p][i] = mx_bias(of_rows, row);
       }
     }
   }
   // to: [COLUMNS / 32][2 steps][64 lanes][8 rows] of a tile
-  __device__ __forceinline__ void store(uint2* to) const {
+  __device__ __forceinline__ void store(u32 row0, u32 end, u32 col0, u32 row_bytes, uint2* to) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       u32 quad, word;
@@ -81,12 +83,13 @@ struct MxUnpack {
       float s[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32 b = scales[p] >> (8 * i) & 255u;
-        s[i] = __uint_as_float(b ? b << 23 : 0x00400000u);
+        // (a row that is out, or behind the last one, has zeros: also where it stands for NaN)
+        const bool in = (col0 + 8 * word) / 2 < row_bytes && row0 + 4 * quad + i < end && !(BIAS && bias[p][i] == -kMxInf);
+        if (!in) codes[p][i] = scales[p][i] = 0;
+        s[i] = __uint_as_float(scales[p][i] ? scales[p][i] << 23 : 0x00400000u);
       }
       // rows 8 k + 4 half + i of a step (16 rows, k = 0, 1) are elements 4 k + i of lane half
       const u32 step = quad / 4, k = quad / 2 % 2, half = quad % 2;
-      uint2* at = to + (((word / 4) * 2 + step) * kWave + half * 32 + word % 4 * 8) * 2 + k;
 #pragma unroll
       for (int c = 0; c < 8; c += 2) {
         u32 two[4];
@@ -99,8 +102,10 @@ struct MxUnpack {
           else v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[p][i], s[i], 3);
           two[i] = __builtin_bit_cast(u32, v);
         }
-        at[2 * c] = make_uint2(__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u));
-        at[2 * c + 2] = make_uint2(__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u));
+        const u32 col = word % 4 * 8 + c;
+        to[mx_unit(word / 4, step, half * 32 + col) * 2 + k] =
+            make_uint2(__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u));
+        to[mx_unit(word / 4, step, half * 32 + col + 1) * 2 + k] = make_uint2(__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u));
       }
     }
   }
@@ -144,30 +149,34 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   const float base = q_lse * kMxLog2e, rest = __fmaf_rn(q_lse, kMxLog2e, -base) + q_lse * 1.92596300e-8f;
   const float correct = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base, -rest));
   float a = 1.f, b = 0.f;
+  // (-1, 0) and (0, -1) in bfloat16, in registers: the second as a constant of the instruction is not what the GPU takes it for
+  u32 minus_low = 0x0000BF80u, minus_high = 0xBF800000u;
+  asm("" : "+v"(minus_low), "+v"(minus_high));
+  MxTile sum[BLOCKS];
+#pragma unroll
+  for (int k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();
+
+  MxUnpack<COLUMNS, BIAS> unpack;
+  unpack.load(rows, first + wave * kMxTile, col0, row_bytes, blocks, bias);
+  MxRow<SHAPE> next;
+  float next_bias = 0.f;
+  u32 next_row = min(first + split * kMxTile + lane % 32, rows.n - 1);
+  if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
+  if (BIAS) next_bias = mx_bias(bias, next_row);
   if (ENTROPY) {
     float u = 0.f;
+#pragma unroll 8
     for (u32 g = half; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)mine * n_given + g, rows.n, bias);
     u += __shfl_xor(u, 32, kWave);
     const float h = d_entropy[mine];
     a = -__fmaf_rn(h, entropy[mine], u);
     b = -h * kMxLn2;
   }
-  MxTile sum[BLOCKS];
-#pragma unroll
-  for (int k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();
-
-  MxUnpack<COLUMNS, BIAS> unpack;
-  unpack.load(rows, first + wave * kMxTile, end, col0, row_bytes, blocks, bias);
-  unpack.store(s_rows[0][wave]);
-  MxRow<SHAPE> next;
-  float next_bias = 0.f;
-  u32 next_row = min(first + split * kMxTile + lane % 32, rows.n - 1);
-  if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
-  if (BIAS) next_bias = mx_bias(bias, next_row);
+  unpack.store(first + wave * kMxTile, end, col0, row_bytes, s_rows[0][wave]);
   __syncthreads();
   u32 buffer = 0;
   for (u32 stage0 = first; stage0 < end; stage0 += kMxStageRows, buffer ^= 1u) {
-    unpack.load(rows, stage0 + kMxStageRows + wave * kMxTile, end, col0, row_bytes, blocks, bias);
+    unpack.load(rows, stage0 + kMxStageRows + wave * kMxTile, col0, row_bytes, blocks, bias);
     for (u32 tile = split; tile < kMxStageTiles; tile += splits) {
       const u32 row0 = stage0 + tile * kMxTile;
       if (row0 >= end) continue;
@@ -178,9 +187,10 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
       const u32 ahead = tile + splits < kMxStageTiles ? row0 + splits * kMxTile : stage0 + kMxStageRows + split * kMxTile;
       next_row = min(ahead + lane % 32, rows.n - 1);
       if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
+      if (BIAS) next_bias = mx_bias(bias, next_row);
+      __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)
       float x_bias[16];
       if (BIAS) {
-        next_bias = mx_bias(bias, next_row);
         if (my_bias == -kMxInf) {
 #pragma unroll
           for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r.scales[w] = 0;
@@ -199,29 +209,29 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
       u32 piece[3][8];            // pairs of rows, first / second / last eight bits of c
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        u32 bits[2][3];
+        float c[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const float t = BIAS ? (__fmaf_rn(d[i + k], scale, x_bias[i + k]) - q_lse) * unit.unit : __fmaf_rn(d[i + k], unit.unit, -base);
-          float c = exp2_fast(t);
+          c[k] = exp2_fast(t);
           // (log p of a row far below, or out, is not multiplied with: its p is 0)
-          if (ENTROPY) c *= __fmaf_rn(b, BIAS ? fmaxf(t, -200.f) : t, a);
-          float left = c;
-#pragma unroll
-          for (int j = 0; j < 3; ++j) {
-            bits[k][j] = __float_as_uint(left);
-            left -= __uint_as_float(bits[k][j] & 0xFFFF0000u);
-          }
+          if (ENTROPY) c[k] *= __fmaf_rn(b, BIAS ? fmaxf(t, -200.f) : t, a);
         }
+        // the upper halves of both, and what they leave, twice: c - 1 x piece in one instruction, exactly
 #pragma unroll
-        for (int j = 0; j < 3; ++j) piece[j][i / 2] = __builtin_amdgcn_perm(bits[1][j], bits[0][j], 0x07060302u);
+        for (int j = 0; j < 3; ++j) {
+          const u32 both = __builtin_amdgcn_perm(__float_as_uint(c[1]), __float_as_uint(c[0]), 0x07060302u);
+          piece[j][i / 2] = both;
+          c[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_low), c[0], false);
+          c[1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_high), c[1], false);
+        }
       }
 #pragma unroll
       for (int step = 0; step < 2; ++step) {
         MxHalves8 value[BLOCKS];
 #pragma unroll
         for (int k = 0; k < BLOCKS; ++k)
-          value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][((k * 2 + step) * kWave + lane) * 2]);
+          value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][mx_unit(k, step, lane) * 2]);
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
           const uint4 w = make_uint4(piece[j][4 * step], piece[j][4 * step + 1], piece[j][4 * step + 2], piece[j][4 * step + 3]);
@@ -231,7 +241,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
         }
       }
     }
-    unpack.store(s_rows[buffer ^ 1u][wave]);
+    unpack.store(stage0 + kMxStageRows + wave * kMxTile, end, col0, row_bytes, s_rows[buffer ^ 1u][wave]);
     __syncthreads();
   }
   if (query >= queries.n) return;

@@ -25,7 +25,8 @@ uint64_t mx_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 // a part share an XCD and with it the L2 that holds its rows.
 constexpr uint64_t kMxWaves = 4096;
 constexpr uint64_t kMxFewQueries = 256;
-constexpr uint64_t kMxGradGroups = 1024;           // workgroups of mx_gradient
+// Workgroups of mx_gradient: as many as run at once (with 64 KB of LDS two on a CU, with 32 four), so that all end together.
+constexpr uint64_t kMxGradGroups = 512;
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
 };
@@ -229,7 +230,7 @@ static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t d
   s.query_groups = mx_ceil(tiles, s.query_tiles);
   s.columns = dim <= 32 ? 32 : dim <= 64 ? 64 : 128;
   s.column_groups = mx_ceil(dim, s.columns);
-  const uint64_t wanted = mx_ceil(std::max<uint64_t>(1, kMxGradGroups / (s.query_groups * s.column_groups)), kXcds) * kXcds;
+  const uint64_t wanted = std::max<uint64_t>(1, kMxGradGroups * (s.columns > 64 ? 1 : 2) / (s.query_groups * s.column_groups));
   s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), kMxStageRows) * kMxStageRows;
   s.parts = mx_ceil(n_rows, s.part_rows);
   s.sums = s.parts * (kMxGradWaves / s.query_tiles);
