@@ -207,22 +207,14 @@ __device__ __forceinline__ int4 mx_load_block(const uint8_t* at) {
   return make_int4(*reinterpret_cast<const int*>(at), 0, 0, 0);
 }
 
-// Loads a lane's blocks of row `row` (below n).  A block that the row does not have (`blocks` is odd, or below 2 *
-// STEPS - 1) is read as the row's last one: the other operand has to be zero there, which mx_clear_rest sees to.
+// The scale bytes of a lane's blocks of row `row` (below n).  A block that the row does not have (`blocks` is odd, or below 2 *
+// STEPS - 1) has some scale, not that of a NaN unless the row has one.
 template <typename SHAPE>
-__device__ __forceinline__ void mx_load_row(const MxHeld& m, u32 row, u32 blocks, MxRow<SHAPE>* to) {
+__device__ __forceinline__ void mx_load_scales(const MxHeld& m, u32 row, u32 blocks, u32* to) {
   const u32 half = lane_id() / 32;
-  if (SHAPE::WIDTH < 16) {
-    to->codes[0] = mx_load_block<SHAPE::WIDTH>(m.codes + (u64)row * SHAPE::WIDTH);
-    to->scales[0] = m.scales[row];
-    return;
-  }
   const u64 first = (u64)row * blocks;
-#pragma unroll
-  for (int s = 0; s < SHAPE::STEPS; ++s)
-    if (s == 0 || 2 * s < (int)blocks) to->codes[s] = mx_load_block<16>(m.codes + (first + min(2 * s + half, blocks - 1)) * 16);
   if (SHAPE::STEPS == 1) {
-    to->scales[0] = m.scales[first + min(half, blocks - 1)];
+    to[0] = m.scales[first + min(half, blocks - 1)];
     return;
   }
   // Eight scale bytes at a time, those of four steps of both halves; where fewer are left in the array, the last
@@ -230,7 +222,7 @@ __device__ __forceinline__ void mx_load_row(const MxHeld& m, u32 row, u32 blocks
   const u64 all = (u64)m.n * blocks;
 #pragma unroll
   for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) {
-    if (8 * w >= (int)blocks) { to->scales[w] = 0; continue; }
+    if (8 * w >= (int)blocks) { to[w] = 0; continue; }
     u64 eight;
     if (all >= 8) {
       const u64 at = first + 8 * w, from = min(at, all - 8);
@@ -240,14 +232,26 @@ __device__ __forceinline__ void mx_load_row(const MxHeld& m, u32 row, u32 blocks
       eight = 0;
       for (u32 i = 0; i < min(8u, blocks - 8 * w); ++i) eight |= (u64)m.scales[first + 8 * w + i] << (8 * i);
     }
-    to->scales[w] = __builtin_amdgcn_perm((u32)(eight >> 32), (u32)eight, half ? 0x07050301u : 0x06040200u);
+    to[w] = __builtin_amdgcn_perm((u32)(eight >> 32), (u32)eight, half ? 0x07050301u : 0x06040200u);
   }
   // (the byte behind the last block of an odd number is another row's, and may stand for NaN)
   if (blocks & 1u) {
 #pragma unroll
     for (int w = 0; w < SHAPE::SCALE_WORDS; ++w)
-      if (half && blocks / 8 == (u32)w) to->scales[w] &= ~(0xFFu << (8 * (blocks / 2 % 4)));
+      if (half && blocks / 8 == (u32)w) to[w] &= ~(0xFFu << (8 * (blocks / 2 % 4)));
   }
+}
+
+// Loads a lane's blocks of row `row` (below n).  A block that the row does not have is read as the row's last one: the
+// other operand has to be zero there, which mx_clear_rest sees to.
+template <typename SHAPE>
+__device__ __forceinline__ void mx_load_row(const MxHeld& m, u32 row, u32 blocks, MxRow<SHAPE>* to) {
+  const u32 half = lane_id() / 32;
+  const u64 first = (u64)row * blocks;
+#pragma unroll
+  for (int s = 0; s < SHAPE::STEPS; ++s)
+    if (s == 0 || 2 * s < (int)blocks) to->codes[s] = mx_load_block<SHAPE::WIDTH>(m.codes + (first + min(2 * s + half, blocks - 1)) * SHAPE::WIDTH);
+  mx_load_scales<SHAPE>(m, row, blocks, to->scales);
 }
 
 // Takes out of an operand what mx_load_row has read in place of blocks that the rows do not have.
@@ -257,6 +261,16 @@ __device__ __forceinline__ void mx_clear_rest(u32 blocks, MxRow<SHAPE>* row) {
 #pragma unroll
   for (int s = 0; s < SHAPE::STEPS; ++s)
     if (2 * s + half >= blocks) row->codes[s] = make_int4(0, 0, 0, 0);
+}
+
+// Changes the signs of all values.
+template <typename SHAPE>
+__device__ __forceinline__ void mx_negate(MxRow<SHAPE>* row) {
+#pragma unroll
+  for (int s = 0; s < SHAPE::STEPS; ++s) {
+    int4& c = row->codes[s];
+    c = make_int4(c.x ^ 0x88888888, c.y ^ 0x88888888, c.z ^ 0x88888888, c.w ^ 0x88888888);
+  }
 }
 
 template <int STEP>
@@ -286,6 +300,46 @@ template <typename SHAPE>
 __device__ __forceinline__ MxTile mx_products(const MxRow<SHAPE>& a, const MxRow<SHAPE>& b, u32 blocks) {
   MxTile d = mx_zero_tile();
   mx_steps<SHAPE>(a, b, blocks, &d);
+  return d;
+}
+
+// A tile of 32 rows that the four waves of a workgroup share: wide rows, which would otherwise come out of the caches once for every
+// wave and step.  Units of 16 bytes, a block of all rows together; the rows of every other block are swapped eight by
+// eight, so that the lanes that store at one time (eight blocks of eight rows) meet all banks.
+template <typename SHAPE>
+struct MxShared {
+  static constexpr int OWN = SHAPE::STEPS / 4;               // units a thread brings: blocks t % 8, 8 + t % 8, ... of row t / 8
+  static constexpr int UNITS = SHAPE::STEPS * 2 * kMxTile;
+  static __device__ __forceinline__ u32 unit(u32 block, u32 row) { return block * kMxTile + (row ^ (block & 1u) << 3); }
+  static __device__ __forceinline__ void load(const MxHeld& m, u32 row0, u32 blocks, int4* own) {
+    const u64 first = (u64)min(row0 + threadIdx.x / 8, m.n - 1) * blocks;
+#pragma unroll
+    for (int j = 0; j < OWN; ++j)
+      if (8 * j < (int)blocks) own[j] = mx_load_block<16>(m.codes + (first + min(8 * j + threadIdx.x % 8, blocks - 1)) * 16);
+  }
+  static __device__ __forceinline__ void store(const int4* own, u32 blocks, int4* tile) {
+#pragma unroll
+    for (int j = 0; j < OWN; ++j)
+      if (8 * j < (int)blocks) tile[unit(8 * j + threadIdx.x % 8, threadIdx.x / 8)] = own[j];
+  }
+  static __device__ __forceinline__ int4 get(const int4* tile, int step) {
+    return tile[unit(2 * step + lane_id() / 32, lane_id() % 32)];
+  }
+};
+
+// The products of a shared tile's rows (the first operand) with others that have zeros behind their blocks.
+template <typename SHAPE, int STEP = 0>
+__device__ __forceinline__ void mx_steps_shared(const int4* tile, const u32* scales, const MxRow<SHAPE>& b, u32 blocks, MxTile* d) {
+  if constexpr (STEP < SHAPE::STEPS) {
+    if (STEP == 0 || 2 * STEP < (int)blocks)
+      *d = mx_step<STEP>(MxShared<SHAPE>::get(tile, STEP), scales[STEP / 4], b.codes[STEP], b.scales[STEP / 4], *d);
+    mx_steps_shared<SHAPE, STEP + 1>(tile, scales, b, blocks, d);
+  }
+}
+template <typename SHAPE>
+__device__ __forceinline__ MxTile mx_products_shared(const int4* tile, const u32* scales, const MxRow<SHAPE>& b, u32 blocks) {
+  MxTile d = mx_zero_tile();
+  mx_steps_shared<SHAPE>(tile, scales, b, blocks, &d);
   return d;
 }
 

@@ -136,13 +136,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   MxRow<SHAPE> q;
   mx_load_row<SHAPE>(queries, mine, blocks, &q);
   mx_clear_rest<SHAPE>(blocks, &q);
-  if (!BIAS && scale < 0.f) {
-#pragma unroll
-    for (int s = 0; s < SHAPE::STEPS; ++s) {
-      int4& c = q.codes[s];
-      c = make_int4(c.x ^ 0x88888888, c.y ^ 0x88888888, c.z ^ 0x88888888, c.w ^ 0x88888888);
-    }
-  }
+  if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
   // (-inf: all rows are out, and any number will do)
   const float q_lse = lse[mine] == -kMxInf ? 0.f : lse[mine];
   // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p

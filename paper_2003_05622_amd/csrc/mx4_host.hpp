@@ -49,7 +49,10 @@ MxSplit mx_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top
   s.groups = top ? mx_ceil(n_rows, s.group) : 0;
   return s;
 }
+// Whether the waves of a workgroup share the rows' tiles: rows of more than 256 values, and queries for at least three of its four waves.
+bool mx_shares_rows(uint64_t n_queries, uint32_t dim) { return mx_blocks(dim) > 8 && n_queries > 2 * kMxTile; }
 MxSplit mx_softmax_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top) {
+  if (mx_shares_rows(n_queries, dim)) return mx_split(n_queries, n_rows, dim, top, kMxThreads / kWave, kMxWaves / (kMxThreads / kWave));
   return mx_split(n_queries, n_rows, dim, top, (uint32_t)mx_wave_tiles(n_queries, dim), kMxWaves);
 }
 size_t mx_parts_bytes(const MxSplit& s, uint64_t n_queries) { return align_up(s.parts * n_queries * sizeof(MxPart)); }
@@ -200,6 +203,10 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
                                                   (u32)p.part_rows, (u32)p.group, (u32)p.groups, parts, highest)
       if constexpr (Shape::STEPS <= 4) {
         if (mx_wave_tiles(m, dim) == 2) { HPS_MX_SOFTMAX(2); return; }
+      } else if (mx_shares_rows(m, dim)) {
+        mx_softmax_shared<Shape, B><<<grid, kMxThreads, 0, s>>>(mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias,
+                                                                (u32)p.part_rows, (u32)p.group, (u32)p.groups, parts, highest);
+        return;
       }
       HPS_MX_SOFTMAX(1);
 #undef HPS_MX_SOFTMAX

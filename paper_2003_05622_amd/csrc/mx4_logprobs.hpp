@@ -113,13 +113,7 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
   for (int k = 0; k < QT; ++k) {
     mx_load_row<SHAPE>(queries, min(query0 + k * kMxTile, queries.n - 1), blocks, &q[k]);
     mx_clear_rest<SHAPE>(blocks, &q[k]);
-    if (!BIAS && scale < 0.f) {
-#pragma unroll
-      for (int s = 0; s < SHAPE::STEPS; ++s) {
-        int4& c = q[k].codes[s];
-        c = make_int4(c.x ^ 0x88888888, c.y ^ 0x88888888, c.z ^ 0x88888888, c.w ^ 0x88888888);
-      }
-    }
+    if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[k]);
     sum[k] = mx_no_part();
     high[k] = -kMxInf;
   }
@@ -181,6 +175,75 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
     const u32 query = query0 + k * kMxTile;
     if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum[k];
   }
+}
+
+// Wide rows and more than a few queries: the four waves of a workgroup hold 32 queries each and share the rows' tiles.
+template <typename SHAPE, bool BIAS>
+__global__ void __launch_bounds__(kMxThreads) HPS_MX_WAVES
+mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, u32 part_rows, u32 group,
+                  u32 n_groups, MxPart* __restrict__ parts, float* __restrict__ highest) {
+  typedef MxShared<SHAPE> Shared;
+  __shared__ int4 s_tile[2][Shared::UNITS];
+  __shared__ float s_bias[2][kMxTile];
+  const u32 lane = lane_id(), half = lane / 32, part = blockIdx.x;
+  const u32 query = (blockIdx.y * (kMxThreads / kWave) + threadIdx.x / kWave) * kMxTile + lane % 32;
+  const u32 first = part * part_rows, end = min(rows.n - first, part_rows) + first;
+  const float unit = BIAS ? kMxLog2e : fabsf(scale) * kMxLog2e;
+  MxRow<SHAPE> q;
+  mx_load_row<SHAPE>(queries, min(query, queries.n - 1), blocks, &q);
+  mx_clear_rest<SHAPE>(blocks, &q);
+  if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
+  MxPart sum = mx_no_part();
+  float high = -kMxInf;
+  int4 own[Shared::OWN];
+  u32 scales[SHAPE::SCALE_WORDS];
+  float my_bias = 0.f;
+  Shared::load(rows, first, blocks, own);
+  mx_load_scales<SHAPE>(rows, min(first + lane % 32, rows.n - 1), blocks, scales);
+  if (BIAS) my_bias = mx_bias(bias, min(first + lane % 32, rows.n - 1));
+  u32 in_group = 0, buffer = 0;
+  for (u32 row0 = first; row0 < end; row0 += kMxTile, buffer ^= 1u) {
+    Shared::store(own, blocks, s_tile[buffer]);
+    u32 r_scales[SHAPE::SCALE_WORDS];
+#pragma unroll
+    for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r_scales[w] = scales[w];
+    if (BIAS) {
+      const float b = row0 + lane % 32 < end ? my_bias : -kMxInf;
+      // a row that is out has products all the same, but none that are NaN
+      if (b == -kMxInf) {
+#pragma unroll
+        for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r_scales[w] = 0;
+      }
+      if (threadIdx.x < kMxTile) s_bias[buffer][lane] = b;
+    }
+    // (a buffer is written two tiles after it was read, and a barrier lies between)
+    __syncthreads();
+    const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
+    Shared::load(rows, row0 + kMxTile, blocks, own);
+    mx_load_scales<SHAPE>(rows, ahead, blocks, scales);
+    if (BIAS) my_bias = mx_bias(bias, ahead);
+    __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)
+    float b[16] = {};
+    if (BIAS) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 v = *reinterpret_cast<const float4*>(&s_bias[buffer][8 * g + 4 * half]);
+        b[4 * g] = v.x; b[4 * g + 1] = v.y; b[4 * g + 2] = v.z; b[4 * g + 3] = v.w;
+      }
+    }
+    const MxTile d = mx_products_shared<SHAPE>(s_tile[buffer], r_scales, q, blocks);
+    if (BIAS || row0 + kMxTile <= end) mx_add_rows<BIAS, false>(d, scale, b, 0, unit, &sum, &high);
+    else mx_add_rows<BIAS, true>(d, scale, b, end - row0, unit, &sum, &high);
+    in_group += kMxTile;
+    if (highest && (in_group == group || row0 + kMxTile >= end)) {
+      in_group = 0;
+      const float h = fmaxf(high, __shfl_xor(high, 32, kWave));
+      if (half == 0 && query < queries.n) highest[(u64)query * n_groups + row0 / group] = h;
+      high = -kMxInf;
+    }
+  }
+  sum = mx_join(sum, mx_shuffle_xor(sum, 32), unit);
+  if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum;
 }
 
 // ---- the best of many, 64 at a time -----------------------------------------------------------

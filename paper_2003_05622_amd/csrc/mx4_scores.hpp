@@ -4,7 +4,7 @@
 // the time that a byte takes.  So the lanes lie along the rows, and a wave's tiles are dealt out so that a lane has
 // neighbouring rows of a query (tile t holds rows RT j + t): a store writes RT neighbouring scores a lane, whole lines a wave.
 // A wave holds RT x 32 rows and goes through the query tiles of its part; the rows' operands stay in
-// registers, the queries', which all waves share, come out of the caches.
+// registers, the queries' come out of the caches, those of wide rows out of LDS, where the waves of a workgroup share them.
 #pragma once
 
 #include "mx4.hpp"
@@ -56,25 +56,20 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
   // neighbouring pieces of work, which share rows, to one XCD
   const u32 piece = xcd_piece(blockIdx.x, gridDim.x), row_group = piece / query_parts, query_part = piece - row_group * query_parts;
   const u32 row0 = (row_group * (kMxThreads / kWave) + wave) * (RT * kMxTile), row = row0 + lane % 32 * RT;
-  if (row0 >= rows.n) return;
+  constexpr bool SHARED = SHAPE::STEPS >= 8;
+  if (!SHARED && row0 >= rows.n) return;
   MxRow<SHAPE> r[RT];
   float b[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const u32 at = min(row + t, rows.n - 1);
     mx_load_row<SHAPE>(rows, at, blocks, &r[t]);
+    mx_clear_rest<SHAPE>(blocks, &r[t]);
     b[t] = BIAS ? mx_bias(bias, at) : 0.f;
   }
   const u32 left = row < rows.n ? min(rows.n - row, (u32)RT) : 0;
-  const u32 tiles = (queries.n + kMxTile - 1) / kMxTile, last = min(query_part * part_tiles + part_tiles, tiles);
-  for (u32 tile = query_part * part_tiles; tile < last; ++tile) {
-    const u32 query0 = tile * kMxTile;
-    MxRow<SHAPE> q;
-    mx_load_row<SHAPE>(queries, min(query0 + lane % 32, queries.n - 1), blocks, &q);
-    mx_clear_rest<SHAPE>(blocks, &q);
-    MxTile d[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) d[t] = mx_products<SHAPE>(q, r[t], blocks);
+  const u32 tiles = (queries.n + kMxTile - 1) / kMxTile, begin = query_part * part_tiles, last = min(begin + part_tiles, tiles);
+  auto store = [&](const MxTile* d, u32 query0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const u32 query = query0 + mx_row_of(i, half);
@@ -83,6 +78,40 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
 #pragma unroll
       for (int t = 0; t < RT; ++t) s[t] = mx_score<BIAS>(d[t][i], scale, b[t]);
       mx_store_scores<RT, BF16>(out, query * stride + row, s, left);
+    }
+  };
+  MxTile d[RT];
+  if constexpr (SHARED) {
+    // (the shared tile is the first operand, and has what lies behind a row's blocks: the rows are without it)
+    typedef MxShared<SHAPE> Shared;
+    __shared__ int4 s_tile[2][SHARED ? Shared::UNITS : 1];
+    int4 own[Shared::OWN];
+    u32 scales[SHAPE::SCALE_WORDS], buffer = 0;
+    Shared::load(queries, begin * kMxTile, blocks, own);
+    mx_load_scales<SHAPE>(queries, min(begin * kMxTile + lane % 32, queries.n - 1), blocks, scales);
+    for (u32 tile = begin; tile < last; ++tile, buffer ^= 1u) {
+      Shared::store(own, blocks, s_tile[buffer]);
+      u32 q_scales[SHAPE::SCALE_WORDS];
+#pragma unroll
+      for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) q_scales[w] = scales[w];
+      __syncthreads();
+      Shared::load(queries, (tile + 1) * kMxTile, blocks, own);
+      mx_load_scales<SHAPE>(queries, min((tile + 1) * kMxTile + lane % 32, queries.n - 1), blocks, scales);
+      __builtin_amdgcn_sched_barrier(0);        // (the loads above are not to be put off until their results are wanted)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) d[t] = mx_products_shared<SHAPE>(s_tile[buffer], q_scales, r[t], blocks);
+      store(d, tile * kMxTile);
+    }
+  } else {
+    MxRow<SHAPE> next;
+    mx_load_row<SHAPE>(queries, min(begin * kMxTile + lane % 32, queries.n - 1), blocks, &next);
+    for (u32 tile = begin; tile < last; ++tile) {
+      const MxRow<SHAPE> q = next;
+      mx_load_row<SHAPE>(queries, min((tile + 1) * kMxTile + lane % 32, queries.n - 1), blocks, &next);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) d[t] = mx_products<SHAPE>(q, r[t], blocks);
+      store(d, tile * kMxTile);
     }
   }
 }
