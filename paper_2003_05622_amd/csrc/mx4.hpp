@@ -166,6 +166,7 @@ mx_get(TableView t, const u64* __restrict__ keys, u64 n_keys, uint8_t* __restric
 typedef int MxOperand __attribute__((ext_vector_type(8)));
 typedef float MxTile __attribute__((ext_vector_type(16)));
 constexpr u32 kMxTile = 32;
+constexpr float kMxInf = __builtin_huge_valf();
 
 __device__ __forceinline__ u32 mx_row_of(u32 r, u32 half) { return 8 * (r >> 2) + 4 * half + (r & 3u); }
 
@@ -362,12 +363,12 @@ __device__ __forceinline__ MxTile mx_products_once(const MxHeld& a, u32 a_row, c
 // A score; a row whose bias is not finite is out, whatever its codes are.
 __device__ __forceinline__ float mx_bias(const float* bias, u32 row) {
   const float b = bias[row];
-  return (__float_as_uint(b) & 0x7F800000u) == 0x7F800000u ? -__builtin_huge_valf() : b;
+  return (__float_as_uint(b) & 0x7F800000u) == 0x7F800000u ? -kMxInf : b;
 }
 template <bool BIAS>
 __device__ __forceinline__ float mx_score(float dot, float scale, float bias) {
   if (!BIAS) return __fmul_rn(dot, scale);
-  return bias == -__builtin_huge_valf() ? bias : __fmaf_rn(dot, scale, bias);
+  return bias == -kMxInf ? bias : __fmaf_rn(dot, scale, bias);
 }
 
 }  // namespace hps

@@ -18,7 +18,6 @@ namespace hps {
 
 constexpr float kMxLog2e = 1.44269504088896340736f;
 constexpr float kMxLn2 = 0.69314718055994530942f;
-constexpr float kMxInf = __builtin_huge_valf();
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }     // (2^x below 2^-126 is 0)
 

@@ -11,26 +11,34 @@
 
 namespace hps {
 
+// Two values as bfloat16, rounded to the nearest, ties to even.
+__device__ __forceinline__ u32 mx_halves(float low, float high) {
+  typedef __bf16 Halves __attribute__((ext_vector_type(2)));
+  typedef float Floats __attribute__((ext_vector_type(2)));
+  const Floats both = {low, high};
+  return __builtin_bit_cast(u32, __builtin_convertvector(both, Halves));
+}
+
 // Stores RT neighbouring scores of a query, of which the first `n` are there.  (The GPU stores words of any alignment.)
 template <int RT, bool BF16>
-__device__ __forceinline__ void mx_store_scores(void* out, u64 at, const float* s, u32 n) {
+__device__ __forceinline__ void mx_store_scores(char* at, const float* s, u32 n) {
   if (BF16) {
     typedef u32 Pairs __attribute__((ext_vector_type(RT / 2), aligned(2)));
-    uint16_t* to = static_cast<uint16_t*>(out) + at;
+    uint16_t* to = reinterpret_cast<uint16_t*>(at);
     if (n == RT) {
       Pairs v;
 #pragma unroll
-      for (int t = 0; t < RT / 2; ++t) v[t] = bf16_nearest(s[2 * t]) | bf16_nearest(s[2 * t + 1]) << 16;
+      for (int t = 0; t < RT / 2; ++t) v[t] = mx_halves(s[2 * t], s[2 * t + 1]);
       __builtin_nontemporal_store(v, reinterpret_cast<Pairs*>(to));
       return;
     }
 #pragma unroll
     for (int t = 0; t < RT; ++t)
-      if (t < (int)n) to[t] = (uint16_t)bf16_nearest(s[t]);
+      if (t < (int)n) to[t] = (uint16_t)mx_halves(s[t], 0.f);
     return;
   }
   typedef float Floats __attribute__((ext_vector_type(RT), aligned(4)));
-  float* to = static_cast<float*>(out) + at;
+  float* to = reinterpret_cast<float*>(at);
   if (n == RT) {
     Floats v;
 #pragma unroll
@@ -66,18 +74,32 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
     mx_load_row<SHAPE>(rows, at, blocks, &r[t]);
     mx_clear_rest<SHAPE>(blocks, &r[t]);
     b[t] = BIAS ? mx_bias(bias, at) : 0.f;
+    // a row that is out has products all the same, but none that are NaN
+    if (BIAS && b[t] == -kMxInf) {
+#pragma unroll
+      for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r[t].scales[w] = 0;
+    }
   }
   const u32 left = row < rows.n ? min(rows.n - row, (u32)RT) : 0;
   const u32 tiles = (queries.n + kMxTile - 1) / kMxTile, begin = query_part * part_tiles, last = min(begin + part_tiles, tiles);
+  const u64 pitch = stride * (BF16 ? 2 : 4);
+  char* const mine = static_cast<char*>(out) + half * 4 * pitch + (u64)row * (BF16 ? 2 : 4);
   auto store = [&](const MxTile* d, u32 query0) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const u32 query = query0 + mx_row_of(i, half);
-      if (query >= queries.n) continue;
+    char* to = mine + query0 * pitch;
+    const u32 queries_left = queries.n - query0;
+    auto one = [&](int i) {
       float s[RT];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) s[t] = mx_score<BIAS>(d[t][i], scale, b[t]);
-      mx_store_scores<RT, BF16>(out, query * stride + row, s, left);
+      for (int t = 0; t < RT; ++t) s[t] = BIAS ? __fmaf_rn(d[t][i], scale, b[t]) : __fmul_rn(d[t][i], scale);
+      mx_store_scores<RT, BF16>(to + (8 * (i / 4) + i % 4) * pitch, s, left);
+    };
+    if (queries_left >= kMxTile) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) one(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (mx_row_of(i, half) < queries_left) one(i);
     }
   };
   MxTile d[RT];
