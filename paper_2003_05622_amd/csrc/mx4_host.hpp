@@ -149,8 +149,13 @@ hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows,
     if (row_groups * parts > kMxMaxBlocks || rows->n * queries->n > kMxMaxScores) { rc = HPS_EINVAL; return; }
     mx_by_flag(d_bias != nullptr, [&](auto biased) {
       mx_by_flag(bf16, [&](auto narrow) {
-        mx_scores<Shape, decltype(biased)::value, decltype(narrow)::value><<<(unsigned)(row_groups * parts), kMxThreads, 0, s>>>(
-            mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, d_out, stride, (u32)row_groups, (u32)parts, (u32)part_tiles);
+        // (1024 x 262 144, float32: 203 us past the L2, 300 through it; 333 x 100 003: 49 us past it, 27 through it)
+        const bool lines = stride * (bf16 ? 2 : 4) % 128 == 0 && mx_aligned(d_out, 128);
+        mx_by_flag(lines, [&](auto whole_lines) {
+          mx_scores<Shape, decltype(biased)::value, decltype(narrow)::value, decltype(whole_lines)::value>
+              <<<(unsigned)(row_groups * parts), kMxThreads, 0, s>>>(mx_held(queries), mx_held(rows), mx_blocks(dim), scale, d_bias, d_out,
+                                                                     stride, (u32)row_groups, (u32)parts, (u32)part_tiles);
+        });
       });
     });
   });

@@ -20,7 +20,12 @@ __device__ __forceinline__ u32 mx_halves(float low, float high) {
 }
 
 // Stores RT neighbouring scores of a query, of which the first `n` are there.  (The GPU stores words of any alignment.)
-template <int RT, bool BF16>
+template <bool PAST_CACHE, typename WORDS>
+__device__ __forceinline__ void mx_store_words(WORDS v, WORDS* to) {
+  if (PAST_CACHE) __builtin_nontemporal_store(v, to);
+  else *to = v;
+}
+template <int RT, bool BF16, bool PAST_CACHE>
 __device__ __forceinline__ void mx_store_scores(char* at, const float* s, u32 n) {
   if (BF16) {
     typedef u32 Pairs __attribute__((ext_vector_type(RT / 2), aligned(2)));
@@ -29,7 +34,7 @@ __device__ __forceinline__ void mx_store_scores(char* at, const float* s, u32 n)
       Pairs v;
 #pragma unroll
       for (int t = 0; t < RT / 2; ++t) v[t] = mx_halves(s[2 * t], s[2 * t + 1]);
-      __builtin_nontemporal_store(v, reinterpret_cast<Pairs*>(to));
+      mx_store_words<PAST_CACHE>(v, reinterpret_cast<Pairs*>(to));
       return;
     }
 #pragma unroll
@@ -43,7 +48,7 @@ __device__ __forceinline__ void mx_store_scores(char* at, const float* s, u32 n)
     Floats v;
 #pragma unroll
     for (int t = 0; t < RT; ++t) v[t] = s[t];
-    __builtin_nontemporal_store(v, reinterpret_cast<Floats*>(to));
+    mx_store_words<PAST_CACHE>(v, reinterpret_cast<Floats*>(to));
     return;
   }
 #pragma unroll
@@ -55,7 +60,9 @@ __device__ __forceinline__ void mx_store_scores(char* at, const float* s, u32 n)
 template <typename SHAPE>
 constexpr int mx_score_tiles() { return SHAPE::STEPS <= 4 ? 4 : 2; }
 
-template <typename SHAPE, bool BIAS, bool BF16>
+// WHOLE_LINES: the scores of every query start on a memory line.  They go past the L2 then, which has better things to hold;
+// else two waves write a line, and the L2 puts it together.
+template <typename SHAPE, bool BIAS, bool BF16, bool WHOLE_LINES>
 __global__ void __launch_bounds__(kMxThreads) HPS_MX_WAVES
 mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, void* __restrict__ out, u64 stride,
           u32 row_groups, u32 query_parts, u32 part_tiles) {
@@ -91,7 +98,7 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
       float s[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) s[t] = BIAS ? __fmaf_rn(d[t][i], scale, b[t]) : __fmul_rn(d[t][i], scale);
-      mx_store_scores<RT, BF16>(to + (8 * (i / 4) + i % 4) * pitch, s, left);
+      mx_store_scores<RT, BF16, WHOLE_LINES>(to + (8 * (i / 4) + i % 4) * pitch, s, left);
     };
     if (queries_left >= kMxTile) {
 #pragma unroll
