@@ -358,66 +358,112 @@ __device__ __forceinline__ float mx_dots(const MxHeld& queries, u32 query, const
   return half ? b[0] : a[0];
 }
 
-// The best groups: every thread takes the best of the groups that fall to it, every wave finds its ceil(top / WAVES) best
-// threads; the worst of these, over all waves, is a bound that `top` groups reach, and hardly more than twice as many do.
-// Those that do are collected and sorted.  The rows of the best groups go the same way, with the last group's highest score as the bound.
+// The largest value of a group of LANES lanes, in all of them.
+template <int LANES, int D = 1>
+__device__ __forceinline__ u64 mx_most(u64 c) {
+  if constexpr (D < LANES) {
+    const u64 o = (u64)mx_lane_xor<D>((u32)(c >> 32)) << 32 | mx_lane_xor<D>((u32)c);
+    return mx_most<LANES, 2 * D>(o > c ? o : c);
+  }
+  return c;
+}
+
+// The best groups: every thread takes the best of the groups that fall to it.  `top` or more sets of threads have a best one each;
+// the worst of these is a bound that `top` groups reach, and some four times as many do at most (where top is above 16, a wave
+// sorts what its threads have and gives its ceil(top / WAVES)-th).  Those that do are collected and sorted.  The rows of the best groups go the
+// same way, with the last group's highest score as the bound.
 template <int WIDTH, bool BIAS, int WAVES>
 __global__ void __launch_bounds__(WAVES * kWave) HPS_MX_WAVES
 mx_finish(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, const MxPart* __restrict__ parts,
           u32 n_parts, const float* __restrict__ highest, u32 group, u32 n_groups, const i32* __restrict__ given, u32 n_given,
           u32 top, float* __restrict__ lse_out, float* __restrict__ entropy_out, float* __restrict__ logp_out,
           i32* __restrict__ top_index, float* __restrict__ top_logp) {
-  constexpr u32 kThreads = WAVES * kWave;
+  constexpr u32 kThreads = WAVES * kWave, kSets = 16;
   __shared__ MxFound<WAVES> s_groups, s_rows;
-  __shared__ MxPart s_part[WAVES];
-  __shared__ u64 s_bound[WAVES];
+  __shared__ float s_m[WAVES], s_l[WAVES], s_e[WAVES];
+  __shared__ u64 s_bound[kSets];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave, query = blockIdx.x;
   const float to_score = BIAS ? 1.f : fabsf(scale), unit = to_score * kMxLog2e;
   const float* mine = highest + (u64)query * n_groups;
+  const MxPart* my_parts = parts + (u64)query * n_parts;
   // (a group without a number among its scores has -inf, also where the scale is 0)
   auto group_candidate = [&](u32 g) {
     const float h = mine[g];
     return mx_candidate(BIAS || h == -kMxInf ? h : __fmul_rn(h, to_score), g);
   };
-  u64 best = 0;
   if (threadIdx.x == 0) s_groups.count = s_rows.count = 0;
+  if (threadIdx.x < kSets) s_bound[threadIdx.x] = ~0ull;
+  float m = kMxLowest;
+#pragma unroll 4
+  for (u32 i = threadIdx.x; i < n_parts; i += kThreads) m = fmaxf(m, my_parts[i].m);
+  u64 best = 0;
   if (top) {
 #pragma unroll 8
     for (u32 g = threadIdx.x; g < n_groups; g += kThreads) {
       const u64 c = group_candidate(g);
       best = c > best ? c : best;
     }
-    const u64 bound = wave_lane(mx_sort(best), (int)((top + WAVES - 1) / WAVES) - 1);
-    if (lane == 0) s_bound[wave] = bound;
   }
-  // join the parts
-  MxPart sum = mx_no_part();
-  for (u32 i = threadIdx.x; i < n_parts; i += kThreads) sum = mx_join(sum, parts[(u64)query * n_parts + i], unit);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) sum = mx_join(sum, mx_shuffle_xor(sum, d), unit);
-  if (lane == 0) s_part[wave] = sum;
   __syncthreads();
   if (top) {
-    u64 bound = s_bound[0];
+    u64 bound;
+    u32 lanes = kWave;
+    if (top <= WAVES) bound = mx_most<64>(best);
+    else if (top <= 2 * WAVES && 2 * WAVES <= (int)kSets) { bound = mx_most<32>(best); lanes = 32; }
+    else if (top <= 4 * WAVES && 4 * WAVES <= (int)kSets) { bound = mx_most<16>(best); lanes = 16; }
+    else bound = wave_lane(mx_sort(best), (int)((top + WAVES - 1) / WAVES) - 1);
+    if (lane % lanes == 0) s_bound[threadIdx.x / lanes] = bound;
+  }
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) bound = s_bound[w] < bound ? s_bound[w] : bound;
+  for (int d = 1; d < kWave; d *= 2) m = fmaxf(m, __shfl_xor(m, d, kWave));
+  if (lane == 0) s_m[wave] = m;
+  __syncthreads();
+  if (top) {
+    const u64 bound = ~mx_most<16>(~s_bound[lane % kSets]);
     if (best >= bound)
       for (u32 g = threadIdx.x; g < n_groups; g += kThreads) {
         const u64 c = group_candidate(g);
         if (c >= bound) s_groups.add(c);
       }
   }
-  sum = s_part[lane % WAVES];
+  // join the parts
+  m = s_m[lane % WAVES];
 #pragma unroll
-  for (int d = 1; d < WAVES; d *= 2) sum = mx_join(sum, mx_shuffle_xor(sum, d), unit);
-  const bool empty = sum.l == 0.f;
-  const float log2_l = log2f(sum.l), lse = empty ? -kMxInf : __fmaf_rn(log2_l, kMxLn2, sum.m * to_score);
+  for (int d = 1; d < WAVES; d *= 2) m = fmaxf(m, __shfl_xor(m, d, kWave));
+  float l = 0.f, e = 0.f;
+  for (u32 i = threadIdx.x; i < n_parts; i += kThreads) {
+    MxPart p = my_parts[i];
+    mx_raise(&p, m, unit);
+    l += p.l;
+    e += p.e;
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    l += __shfl_xor(l, d, kWave);
+    e += __shfl_xor(e, d, kWave);
+  }
+  if (lane == 0) { s_l[wave] = l; s_e[wave] = e; }
+  __syncthreads();
+  l = e = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) { l += s_l[w]; e += s_e[w]; }
+  const bool empty = l == 0.f;
+  const float log2_l = log2f(l), lse = empty ? -kMxInf : __fmaf_rn(log2_l, kMxLn2, m * to_score);
   if (threadIdx.x == 0) {
     lse_out[query] = lse;
-    entropy_out[query] = empty ? 0.f : (log2_l - sum.e / sum.l) * kMxLn2;
+    entropy_out[query] = empty ? 0.f : (log2_l - e / l) * kMxLn2;
+  }
+  // the given rows, by the last waves first
+  for (u32 i0 = (WAVES - 1 - wave) * kWave; i0 < n_given; i0 += kThreads) {
+    const u32 i = i0 + lane;
+    const i32 g = i < n_given ? given[(u64)query * n_given + i] : -1;
+    const bool in = g >= 0 && (u32)g < rows.n;
+    const u32 at = in ? (u32)g : rows.n - 1;
+    const float s = mx_score<BIAS>(mx_dots<WIDTH>(queries, query, rows, at, blocks), scale, BIAS ? mx_bias(bias, at) : 0.f);
+    if (i < n_given)
+      logp_out[(u64)query * n_given + i] = g < 0 ? 0.f : !in ? __uint_as_float(0x7FC00000u) : s == -kMxInf ? s : s - lse;
   }
   if (top) {
-    __syncthreads();
     u32 n = s_groups.count;
     u64 list = 0;
     if (n <= kThreads) {
@@ -463,15 +509,6 @@ mx_finish(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
         top_logp[(u64)query * top + lane] = list ? mx_candidate_score(list) - lse : -kMxInf;
       }
     }
-  }
-  for (u32 i0 = wave * kWave; i0 < n_given; i0 += kThreads) {
-    const u32 i = i0 + lane;
-    const i32 g = i < n_given ? given[(u64)query * n_given + i] : -1;
-    const bool in = g >= 0 && (u32)g < rows.n;
-    const u32 at = in ? (u32)g : rows.n - 1;
-    const float s = mx_score<BIAS>(mx_dots<WIDTH>(queries, query, rows, at, blocks), scale, BIAS ? mx_bias(bias, at) : 0.f);
-    if (i < n_given)
-      logp_out[(u64)query * n_given + i] = g < 0 ? 0.f : !in ? __uint_as_float(0x7FC00000u) : s == -kMxInf ? s : s - lse;
   }
 }
 
