@@ -13,6 +13,7 @@ kept between calls.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 from .binding import EINVAL, OK, HpsError, Mx4Operand, _ptr, lib
@@ -20,6 +21,7 @@ from .binding import EINVAL, OK, HpsError, Mx4Operand, _ptr, lib
 MX4_MAX_TOP = 64
 
 
+@functools.lru_cache(maxsize=None)
 def _row_shape(dim: int):
     """(bytes of codes, bytes of scales) of a row."""
     if dim < 4 or dim > 1024 or dim % 4:
@@ -69,6 +71,12 @@ class Mx4Rows:
         out = torch.empty((self.n, self.dim), dtype=torch.float32, device=self.device)
         _call("hps_mx4_dequantize", self.device, self._operand(), self.dim, out.data_ptr())
         return out
+
+
+@functools.lru_cache(maxsize=256)
+def _space(name: str, *sizes) -> int:
+    """Bytes of workspace a call of these sizes needs."""
+    return getattr(lib(), name)(*sizes)
 
 
 def _call(name: str, device, *args) -> None:
@@ -170,7 +178,7 @@ def mx4_logprobs(queries: Mx4Rows, rows: Mx4Rows, given=None, top: int = 0, scal
     logp = torch.empty((m, g), dtype=torch.float32, device=device) if given is not None else None
     index = torch.empty((m, top), dtype=torch.int32, device=device) if top else None
     best = torch.empty((m, top), dtype=torch.float32, device=device) if top else None
-    size = lib().hps_mx4_logprobs_bytes(m, n, dim, top)
+    size = _space("hps_mx4_logprobs_bytes", m, n, dim, top)
     space = torch.empty(size, dtype=torch.uint8, device=device)
     _call("hps_mx4_logprobs", device, queries._operand(), rows._operand(), dim, scale, _array(bias, "bias", torch.float32, (n,), device), asked,
           g, top, lse.data_ptr(), entropy.data_ptr(), _ptr(logp), _ptr(index), _ptr(best), space.data_ptr(), size)
@@ -195,7 +203,7 @@ def mx4_logprobs_backward(queries: Mx4Rows, rows: Mx4Rows, given, d_logp, lse, e
             _array(entropy, "entropy", torch.float32, (m,), device), asked, _array(d_logp, "d_logp", torch.float32, (m, g), device), g,
             _array(d_entropy, "d_entropy", torch.float32, (m,), device))
     out = torch.empty((m, dim), dtype=torch.float32, device=device)
-    size = lib().hps_mx4_logprobs_backward_bytes(m, n, dim)
+    size = _space("hps_mx4_logprobs_backward_bytes", m, n, dim)
     space = torch.empty(size, dtype=torch.uint8, device=device)
     _call("hps_mx4_logprobs_backward", device, queries._operand(), rows._operand(), dim, scale, *args, out.data_ptr(), space.data_ptr(),
           size)
