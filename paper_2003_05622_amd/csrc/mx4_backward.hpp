@@ -117,38 +117,21 @@ struct MxGradUnit {
   float off;         // the part of it that float32 does not hold, relative
 };
 
-// A workgroup: query_tiles (1, 2 or 4) x 32 queries, a part of the rows, of which each of 4 / query_tiles groups of waves
+// A workgroup: query_groups (1, 2 or 4) x QT x 32 queries, a part of the rows, of which each of 4 / query_groups groups of waves
 // takes some tiles of every stage (and has a part of its own in `parts`), and COLUMNS columns.
-template <typename SHAPE, bool BIAS, bool ENTROPY, int COLUMNS>
+template <typename SHAPE, bool BIAS, bool ENTROPY, int COLUMNS, int QT>
 __global__ void __launch_bounds__(kMxGradWaves * kWave) HPS_MX_WAVES
 mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, MxGradUnit unit, const float* __restrict__ bias,
             const float* __restrict__ lse, const float* __restrict__ entropy, const i32* __restrict__ given, const float* __restrict__ d_logp,
-            u32 n_given, const float* __restrict__ d_entropy, u32 query_tiles, u32 part_rows, float* __restrict__ parts) {
+            u32 n_given, const float* __restrict__ d_entropy, u32 query_groups, u32 part_rows, float* __restrict__ parts) {
   constexpr int BLOCKS = COLUMNS / 32;
   constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;           // of 8 bytes, a tile's unpacked values
   __shared__ uint2 s_rows[2][kMxStageTiles][kTileWords];
   __shared__ float s_bias[kMxGradWaves][kMxTile];
   const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const u32 splits = kMxGradWaves / query_tiles, split = wave / query_tiles;
-  const u32 query = (blockIdx.y * query_tiles + wave % query_tiles) * kMxTile + lane % 32, mine = min(query, queries.n - 1);
+  const u32 splits = kMxGradWaves / query_groups, split = wave / query_groups;
+  const u32 query0 = (blockIdx.y * query_groups + wave % query_groups) * (QT * kMxTile) + lane % 32;
   const u32 first = blockIdx.x * part_rows, end = min(rows.n - first, part_rows) + first, col0 = blockIdx.z * COLUMNS;
-
-  MxRow<SHAPE> q;
-  mx_load_row<SHAPE>(queries, mine, blocks, &q);
-  mx_clear_rest<SHAPE>(blocks, &q);
-  if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
-  // (-inf: all rows are out, and any number will do)
-  const float q_lse = lse[mine] == -kMxInf ? 0.f : lse[mine];
-  // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p
-  const float base = q_lse * kMxLog2e, rest = __fmaf_rn(q_lse, kMxLog2e, -base) + q_lse * 1.92596300e-8f;
-  const float correct = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base, -rest));
-  float a = 1.f, b = 0.f;
-  // (-1, 0) and (0, -1) in bfloat16, in registers: the second as a constant of the instruction is not what the GPU takes it for
-  u32 minus_low = 0x0000BF80u, minus_high = 0xBF800000u;
-  asm("" : "+v"(minus_low), "+v"(minus_high));
-  MxTile sum[BLOCKS];
-#pragma unroll
-  for (int k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();
 
   MxUnpack<COLUMNS, BIAS> unpack;
   unpack.load(rows, first + wave * kMxTile, col0, row_bytes, blocks, bias);
@@ -157,15 +140,38 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   u32 next_row = min(first + split * kMxTile + lane % 32, rows.n - 1);
   if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
   if (BIAS) next_bias = mx_bias(bias, next_row);
-  if (ENTROPY) {
-    float u = 0.f;
+
+  MxRow<SHAPE> q[QT];
+  float q_lse[QT], base[QT], correct[QT], a[QT], b[QT];
+  MxTile sum[QT][BLOCKS];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const u32 mine = min(query0 + t * kMxTile, queries.n - 1);
+    mx_load_row<SHAPE>(queries, mine, blocks, &q[t]);
+    mx_clear_rest<SHAPE>(blocks, &q[t]);
+    if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[t]);
+    // (-inf: all rows are out, and any number will do)
+    q_lse[t] = lse[mine] == -kMxInf ? 0.f : lse[mine];
+    // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p
+    base[t] = q_lse[t] * kMxLog2e;
+    const float rest = __fmaf_rn(q_lse[t], kMxLog2e, -base[t]) + q_lse[t] * 1.92596300e-8f;
+    correct[t] = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base[t], -rest));
+    if (ENTROPY) {
+      float u = 0.f;
 #pragma unroll 8
-    for (u32 g = half; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)mine * n_given + g, rows.n, bias);
-    u += __shfl_xor(u, 32, kWave);
-    const float h = d_entropy[mine];
-    a = -__fmaf_rn(h, entropy[mine], u);
-    b = -h * kMxLn2;
+      for (u32 g = half; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)mine * n_given + g, rows.n, bias);
+      u += __shfl_xor(u, 32, kWave);
+      const float h = d_entropy[mine];
+      a[t] = -__fmaf_rn(h, entropy[mine], u);
+      b[t] = -h * kMxLn2;
+    }
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) sum[t][k] = mx_zero_tile();
   }
+  // (-1, 0) and (0, -1) in bfloat16, in registers: the second as a constant of the instruction is not what the GPU takes it for
+  u32 minus_low = 0x0000BF80u, minus_high = 0xBF800000u;
+  asm("" : "+v"(minus_low), "+v"(minus_high));
+
   unpack.store(first + wave * kMxTile, end, col0, row_bytes, s_rows[0][wave]);
   __syncthreads();
   u32 buffer = 0;
@@ -199,27 +205,9 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
           x_bias[4 * g] = v.x; x_bias[4 * g + 1] = v.y; x_bias[4 * g + 2] = v.z; x_bias[4 * g + 3] = v.w;
         }
       }
-      const MxTile d = mx_products<SHAPE>(r, q, blocks);
-      u32 piece[3][8];            // pairs of rows, first / second / last eight bits of c
+      MxTile d[QT];
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        float c[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float t = BIAS ? (__fmaf_rn(d[i + k], scale, x_bias[i + k]) - q_lse) * unit.unit : __fmaf_rn(d[i + k], unit.unit, -base);
-          c[k] = exp2_fast(t);
-          // (log p of a row far below, or out, is not multiplied with: its p is 0)
-          if (ENTROPY) c[k] *= __fmaf_rn(b, BIAS ? fmaxf(t, -200.f) : t, a);
-        }
-        // the upper halves of both, and what they leave, twice: c - 1 x piece in one instruction, exactly
-#pragma unroll
-        for (int j = 0; j < 3; ++j) {
-          const u32 both = __builtin_amdgcn_perm(__float_as_uint(c[1]), __float_as_uint(c[0]), 0x07060302u);
-          piece[j][i / 2] = both;
-          c[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_low), c[0], false);
-          c[1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_high), c[1], false);
-        }
-      }
+      for (int t = 0; t < QT; ++t) d[t] = mx_products<SHAPE>(r, q[t], blocks);
 #pragma unroll
       for (int step = 0; step < 2; ++step) {
         MxHalves8 value[BLOCKS];
@@ -227,28 +215,57 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
         for (int k = 0; k < BLOCKS; ++k)
           value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][mx_unit(k, step, lane) * 2]);
 #pragma unroll
-        for (int j = 0; j < 3; ++j) {
-          const uint4 w = make_uint4(piece[j][4 * step], piece[j][4 * step + 1], piece[j][4 * step + 2], piece[j][4 * step + 3]);
+        for (int t = 0; t < QT; ++t) {
+          u32 piece[3][4];            // pairs of rows, first / second / last eight bits of c
 #pragma unroll
-          for (int k = 0; k < BLOCKS; ++k)
-            sum[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[k], 0, 0, 0);
+          for (int i = 0; i < 8; i += 2) {
+            float c[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int at = 8 * step + i + k;
+              const float x = d[t][at];
+              const float p = BIAS ? (__fmaf_rn(x, scale, x_bias[at]) - q_lse[t]) * unit.unit : __fmaf_rn(x, unit.unit, -base[t]);
+              c[k] = exp2_fast(p);
+              // (log p of a row far below, or out, is not multiplied with: its p is 0)
+              if (ENTROPY) c[k] *= __fmaf_rn(b[t], BIAS ? fmaxf(p, -200.f) : p, a[t]);
+            }
+            // the upper halves of both, and what they leave, twice: c - 1 x piece in one instruction, exactly
+#pragma unroll
+            for (int j = 0; j < 3; ++j) {
+              const u32 both = __builtin_amdgcn_perm(__float_as_uint(c[1]), __float_as_uint(c[0]), 0x07060302u);
+              piece[j][i / 2] = both;
+              c[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_low), c[0], false);
+              c[1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_high), c[1], false);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 3; ++j) {
+            const uint4 w = make_uint4(piece[j][0], piece[j][1], piece[j][2], piece[j][3]);
+#pragma unroll
+            for (int k = 0; k < BLOCKS; ++k)
+              sum[t][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[t][k], 0, 0, 0);
+          }
         }
       }
     }
     unpack.store(stage0 + kMxStageRows + wave * kMxTile, end, col0, row_bytes, s_rows[buffer ^ 1u][wave]);
     __syncthreads();
   }
-  if (query >= queries.n) return;
-  float* to = parts + ((u64)(blockIdx.x * splits + split) * queries.n + query) * dim;
 #pragma unroll
-  for (int k = 0; k < BLOCKS; ++k)
+  for (int t = 0; t < QT; ++t) {
+    const u32 query = query0 + t * kMxTile;
+    if (query >= queries.n) continue;
+    float* to = parts + ((u64)(blockIdx.x * splits + split) * queries.n + query) * dim;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const u32 col = col0 + k * 32 + 8 * g + 4 * half;
-      if (col < dim)
-        *reinterpret_cast<float4*>(to + col) = make_float4(sum[k][4 * g] * correct, sum[k][4 * g + 1] * correct, sum[k][4 * g + 2] * correct,
-                                                           sum[k][4 * g + 3] * correct);
-    }
+    for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const u32 col = col0 + k * 32 + 8 * g + 4 * half;
+        if (col < dim)
+          *reinterpret_cast<float4*>(to + col) = make_float4(sum[t][k][4 * g] * correct[t], sum[t][k][4 * g + 1] * correct[t],
+                                                             sum[t][k][4 * g + 2] * correct[t], sum[t][k][4 * g + 3] * correct[t]);
+      }
+  }
 }
 
 // The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.

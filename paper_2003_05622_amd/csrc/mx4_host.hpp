@@ -25,7 +25,7 @@ uint64_t mx_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 // a part share an XCD and with it the L2 that holds its rows.
 constexpr uint64_t kMxWaves = 4096;
 constexpr uint64_t kMxFewQueries = 256;
-// Workgroups of mx_gradient: as many as run at once (with 64 KB of LDS two on a CU, with 32 four), so that all end together.
+// Workgroups of mx_gradient: as many as run at once (two on a CU, four of the narrow ones with one query tile a wave), so that all end together.
 constexpr uint64_t kMxGradGroups = 512;
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
@@ -231,21 +231,24 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
 }
 
-// The gradient's division: workgroups of 128 queries (fewer queries: the waves share the rows instead) and a part of the rows each.
+// The gradient's division: workgroups of up to four (narrow rows and many queries: eight) query tiles and a part of the rows each;
+// where the tiles are fewer than a workgroup's waves, these share the rows instead.
 struct MxGradSplit {
-  uint64_t query_tiles, query_groups, columns, column_groups, part_rows, parts, sums;
+  uint64_t wave_tiles, query_groups, grid_queries, columns, grid_columns, part_rows, parts, sums;
 };
 static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
   MxGradSplit s;
   const uint64_t tiles = mx_ceil(n_queries, kMxTile);
-  s.query_tiles = tiles > 2 ? 4 : tiles;
-  s.query_groups = mx_ceil(tiles, s.query_tiles);
+  s.wave_tiles = dim <= 64 && tiles > 6 ? 2 : 1;
+  const uint64_t waves = mx_ceil(tiles, s.wave_tiles);
+  s.query_groups = waves > 2 ? 4 : waves;
+  s.grid_queries = mx_ceil(waves, s.query_groups);
   s.columns = dim <= 32 ? 32 : dim <= 64 ? 64 : 128;
-  s.column_groups = mx_ceil(dim, s.columns);
-  const uint64_t wanted = std::max<uint64_t>(1, kMxGradGroups * (s.columns > 64 ? 1 : 2) / (s.query_groups * s.column_groups));
+  s.grid_columns = mx_ceil(dim, s.columns);
+  const uint64_t wanted = std::max<uint64_t>(1, kMxGradGroups * (s.columns > 64 || s.wave_tiles == 2 ? 1 : 2) / (s.grid_queries * s.grid_columns));
   s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), kMxStageRows) * kMxStageRows;
   s.parts = mx_ceil(n_rows, s.part_rows);
-  s.sums = s.parts * (kMxGradWaves / s.query_tiles);
+  s.sums = s.parts * (kMxGradWaves / s.query_groups);
   return s;
 }
 
@@ -282,18 +285,19 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
         const double exact = B ? 1.4426950408889634 : std::fabs((double)scale) * 1.4426950408889634;
         const float held = B ? kMxLog2e : std::fabs(scale) * kMxLog2e;
         const MxGradUnit unit = {held, held > 0.f ? (float)(exact / held - 1.0) : 0.f};
-        const dim3 grid((unsigned)p.parts, (unsigned)p.query_groups, (unsigned)p.column_groups);
+        const dim3 grid((unsigned)p.parts, (unsigned)p.grid_queries, (unsigned)p.grid_columns);
         mx_by_shape(dim, [&](auto shape) {
           typedef decltype(shape) Shape;
-          constexpr int COLUMNS = Shape::WIDTH < 16 ? 32 : Shape::STEPS == 1 ? 64 : 128;
-#define HPS_MX_GRADIENT(COLUMNS)                                                                                             \
-  mx_gradient<Shape, B, E, COLUMNS><<<grid, kMxGradWaves * kWave, 0, s>>>(                                                   \
+#define HPS_MX_GRADIENT(COLUMNS, QT)                                                                                         \
+  mx_gradient<Shape, B, E, COLUMNS, QT><<<grid, kMxGradWaves * kWave, 0, s>>>(                                               \
       mx_held(queries), mx_held(rows), dim, blocks, row_bytes, scale, unit, d_bias, d_lse, d_entropy, d_given, d_dlogp,      \
-      n_given, d_dentropy, (u32)p.query_tiles, (u32)p.part_rows, parts)
-          if constexpr (Shape::WIDTH == 16 && Shape::STEPS == 1) {
-            if (p.columns == 32) { HPS_MX_GRADIENT(32); return; }
+      n_given, d_dentropy, (u32)p.query_groups, (u32)p.part_rows, parts)
+          if constexpr (Shape::STEPS > 1) {
+            HPS_MX_GRADIENT(128, 1);
+          } else {
+            if (p.columns == 32) { if (p.wave_tiles == 2) HPS_MX_GRADIENT(32, 2); else HPS_MX_GRADIENT(32, 1); }
+            else if constexpr (Shape::WIDTH == 16) { if (p.wave_tiles == 2) HPS_MX_GRADIENT(64, 2); else HPS_MX_GRADIENT(64, 1); }
           }
-          HPS_MX_GRADIENT(COLUMNS);
 #undef HPS_MX_GRADIENT
         });
       }
