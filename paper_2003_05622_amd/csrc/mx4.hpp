@@ -360,6 +360,14 @@ __device__ __forceinline__ MxTile mx_products_once(const MxHeld& a, u32 a_row, c
   return d;
 }
 
+// Two values as bfloat16, rounded to the nearest, ties to even.
+__device__ __forceinline__ u32 mx_halves(float low, float high) {
+  typedef __bf16 Halves __attribute__((ext_vector_type(2)));
+  typedef float Floats __attribute__((ext_vector_type(2)));
+  const Floats both = {low, high};
+  return __builtin_bit_cast(u32, __builtin_convertvector(both, Halves));
+}
+
 // A score; a row whose bias is not finite is out, whatever its codes are.
 __device__ __forceinline__ float mx_bias(const float* bias, u32 row) {
   const float b = bias[row];

@@ -8,8 +8,11 @@
 // query, c of which is at once the second operand of the product with the rows' values (which rows a step of the
 // matrix instruction takes, in which order, is free as long as both operands agree).  The values, exact in
 // bfloat16, are unpacked into LDS by the workgroup, in the order the first operand wants them: lane l of a step holds
-// column l % 32 of eight rows.  c goes through the matrix instruction in three bfloat16 pieces that add up
-// to its 24 bits exactly: the sum over the rows is what little is left of large terms, and eight bits would show.
+// column l % 32 of eight rows.  c goes through the matrix instruction in bfloat16 pieces: the sum over the rows, together
+// with the given ones, is what little is left of large terms, and eight bits would show.  Three pieces add up to c's 24 bits
+// exactly, two are off by 2^-18 of it at most.  Where p is above 2^-6 all three are used, which a query has at most 64 rows for;
+// the others' errors, independent of each other, come to 2^-18 sqrt(sum p^2) <= 2^-21 of a row at most, as float32 itself
+// leaves (lse is a float32 number: a p is off by 2^-24 |lse| of itself).
 // Without a gradient of the entropy c is p up to a factor per query, which the end applies.
 // mx_gradient_end adds the parts of the rows and the given rows.
 #pragma once
@@ -21,6 +24,7 @@ namespace hps {
 constexpr u32 kMxStageTiles = 4;                         // tiles of 32 rows unpacked at a time
 constexpr u32 kMxStageRows = kMxStageTiles * kMxTile;
 constexpr u32 kMxGradWaves = 4;
+constexpr float kMxLarge = 0x1p-6f;
 
 typedef __bf16 MxHalves2 __attribute__((ext_vector_type(2)));
 typedef __bf16 MxHalves8 __attribute__((ext_vector_type(8)));
@@ -209,41 +213,56 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
 #pragma unroll
       for (int t = 0; t < QT; ++t) d[t] = mx_products<SHAPE>(r, q[t], blocks);
 #pragma unroll
-      for (int step = 0; step < 2; ++step) {
-        MxHalves8 value[BLOCKS];
+      for (int t = 0; t < QT; ++t) {
+        float most = 0.f;
 #pragma unroll
-        for (int k = 0; k < BLOCKS; ++k)
-          value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][mx_unit(k, step, lane) * 2]);
+        for (int i = 0; i < 16; ++i) {
+          const float x = d[t][i];
+          const float log2_p = BIAS ? (__fmaf_rn(x, scale, x_bias[i]) - q_lse[t]) * unit.unit : __fmaf_rn(x, unit.unit, -base[t]);
+          const float p = exp2_fast(log2_p);
+          most = fmaxf(most, p);
+          // (log p of a row far below, or out, is not multiplied with: its p is 0)
+          d[t][i] = ENTROPY ? p * __fmaf_rn(b[t], BIAS ? fmaxf(log2_p, -200.f) : log2_p, a[t]) : p;
+        }
+        const bool all_pieces = __any(most > kMxLarge);
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          u32 piece[3][4];            // pairs of rows, first / second / last eight bits of c
+        for (int step = 0; step < 2; ++step) {
+          MxHalves8 value[BLOCKS];
 #pragma unroll
-          for (int i = 0; i < 8; i += 2) {
-            float c[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const int at = 8 * step + i + k;
-              const float x = d[t][at];
-              const float p = BIAS ? (__fmaf_rn(x, scale, x_bias[at]) - q_lse[t]) * unit.unit : __fmaf_rn(x, unit.unit, -base[t]);
-              c[k] = exp2_fast(p);
-              // (log p of a row far below, or out, is not multiplied with: its p is 0)
-              if (ENTROPY) c[k] *= __fmaf_rn(b[t], BIAS ? fmaxf(p, -200.f) : p, a[t]);
-            }
-            // the upper halves of both, and what they leave, twice: c - 1 x piece in one instruction, exactly
-#pragma unroll
-            for (int j = 0; j < 3; ++j) {
-              const u32 both = __builtin_amdgcn_perm(__float_as_uint(c[1]), __float_as_uint(c[0]), 0x07060302u);
-              piece[j][i / 2] = both;
-              c[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_low), c[0], false);
-              c[1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(MxHalves2, both), __builtin_bit_cast(MxHalves2, minus_high), c[1], false);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 3; ++j) {
-            const uint4 w = make_uint4(piece[j][0], piece[j][1], piece[j][2], piece[j][3]);
+          for (int k = 0; k < BLOCKS; ++k)
+            value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][mx_unit(k, step, lane) * 2]);
+          auto add = [&](const u32* piece) {
+            const uint4 w = make_uint4(piece[0], piece[1], piece[2], piece[3]);
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k)
               sum[t][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[t][k], 0, 0, 0);
+          };
+          // pairs of rows: the upper halves of both; what they leave (c - 1 x piece in one instruction, exactly), rounded;
+          // and what that leaves
+          float c[8];
+          u32 piece[4];
+          auto take_off = [&] {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              const MxHalves2 both = __builtin_bit_cast(MxHalves2, piece[i / 2]);
+              c[i] = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(MxHalves2, minus_low), c[i], false);
+              c[i + 1] = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(MxHalves2, minus_high), c[i + 1], false);
+            }
+          };
+#pragma unroll
+          for (int i = 0; i < 8; ++i) c[i] = d[t][8 * step + i];
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) piece[i / 2] = __builtin_amdgcn_perm(__float_as_uint(c[i + 1]), __float_as_uint(c[i]), 0x07060302u);
+          add(piece);
+          take_off();
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+          add(piece);
+          if (all_pieces) {
+            take_off();
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+            add(piece);
           }
         }
       }

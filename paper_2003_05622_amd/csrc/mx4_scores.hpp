@@ -11,14 +11,6 @@
 
 namespace hps {
 
-// Two values as bfloat16, rounded to the nearest, ties to even.
-__device__ __forceinline__ u32 mx_halves(float low, float high) {
-  typedef __bf16 Halves __attribute__((ext_vector_type(2)));
-  typedef float Floats __attribute__((ext_vector_type(2)));
-  const Floats both = {low, high};
-  return __builtin_bit_cast(u32, __builtin_convertvector(both, Halves));
-}
-
 // Stores RT neighbouring scores of a query, of which the first `n` are there.  (The GPU stores words of any alignment.)
 template <bool PAST_CACHE, typename WORDS>
 __device__ __forceinline__ void mx_store_words(WORDS v, WORDS* to) {
