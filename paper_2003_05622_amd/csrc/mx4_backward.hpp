@@ -121,6 +121,110 @@ struct MxGradUnit {
   float off;         // the part of it that float32 does not hold, relative
 };
 
+// What a lane knows of its query.
+template <bool BIAS>
+struct MxGradQuery {
+  float lse, base, correct, a, b;
+  // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p
+  __device__ __forceinline__ void load(u32 query, const MxGradUnit& unit, const float* of_lse) {
+    // (-inf: all rows are out, and any number will do)
+    lse = of_lse[query] == -kMxInf ? 0.f : of_lse[query];
+    base = lse * kMxLog2e;
+    const float rest = __fmaf_rn(lse, kMxLog2e, -base) + lse * 1.92596300e-8f;
+    correct = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base, -rest));
+    a = 1.f;
+    b = 0.f;
+  }
+  // With a gradient of the entropy: c = p (a + b log2 p).
+  __device__ __forceinline__ void load_entropy(u32 query, const float* entropy, const float* d_entropy, const i32* given, const float* d_logp,
+                                               u32 n_given, u32 n_rows, const float* bias) {
+    float u = 0.f;
+#pragma unroll 8
+    for (u32 g = lane_id() / 32; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)query * n_given + g, n_rows, bias);
+    u += __shfl_xor(u, 32, kWave);
+    const float h = d_entropy[query];
+    a = -__fmaf_rn(h, entropy[query], u);
+    b = -h * kMxLn2;
+  }
+};
+
+// (-1, 0) and (0, -1) in bfloat16, in registers: the second as a constant of the instruction is not what the GPU takes it for.
+struct MxOnes {
+  u32 minus_low = 0x0000BF80u, minus_high = 0xBF800000u;
+  __device__ __forceinline__ MxOnes() { asm("" : "+v"(minus_low), "+v"(minus_high)); }
+};
+
+// Adds c row of 32 rows to the sums of 32 queries.  d: their products; values: the rows' unpacked columns.
+template <bool BIAS, bool ENTROPY, int BLOCKS>
+__device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float scale, const MxGradQuery<BIAS>& query, float unit,
+                                            const uint2* values, const MxOnes& ones, MxTile* sum) {
+  const u32 lane = lane_id();
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float log2_p = BIAS ? (__fmaf_rn(d[i], scale, x_bias[i]) - query.lse) * unit : __fmaf_rn(d[i], unit, -query.base);
+    const float p = exp2_fast(log2_p);
+    most = fmaxf(most, p);
+    // (log p of a row far below, or out, is not multiplied with: its p is 0)
+    d[i] = ENTROPY ? p * __fmaf_rn(query.b, BIAS ? fmaxf(log2_p, -200.f) : log2_p, query.a) : p;
+  }
+  const bool all_pieces = __any(most > kMxLarge);
+#pragma unroll
+  for (int step = 0; step < 2; ++step) {
+    MxHalves8 value[BLOCKS];
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) value[k] = *reinterpret_cast<const MxHalves8*>(&values[mx_unit(k, step, lane) * 2]);
+    auto add = [&](const u32* piece) {
+      const uint4 w = make_uint4(piece[0], piece[1], piece[2], piece[3]);
+#pragma unroll
+      for (int k = 0; k < BLOCKS; ++k)
+        sum[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[k], 0, 0, 0);
+    };
+    // pairs of rows: the upper halves of both; what they leave (c - 1 x piece in one instruction, exactly), rounded;
+    // and what that leaves
+    float c[8];
+    u32 piece[4];
+    auto take_off = [&] {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const MxHalves2 both = __builtin_bit_cast(MxHalves2, piece[i / 2]);
+        c[i] = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(MxHalves2, ones.minus_low), c[i], false);
+        c[i + 1] = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(MxHalves2, ones.minus_high), c[i + 1], false);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = d[8 * step + i];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) piece[i / 2] = __builtin_amdgcn_perm(__float_as_uint(c[i + 1]), __float_as_uint(c[i]), 0x07060302u);
+    add(piece);
+    take_off();
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+    add(piece);
+    if (all_pieces) {
+      take_off();
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+      add(piece);
+    }
+  }
+}
+
+// Writes a query's sums of COLUMNS columns.
+template <int BLOCKS>
+__device__ __forceinline__ void mx_store_sums(const MxTile* sum, float correct, u32 col0, u32 dim, float* to) {
+  const u32 half = lane_id() / 32;
+#pragma unroll
+  for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const u32 col = col0 + k * 32 + 8 * g + 4 * half;
+      if (col < dim)
+        *reinterpret_cast<float4*>(to + col) =
+            make_float4(sum[k][4 * g] * correct, sum[k][4 * g + 1] * correct, sum[k][4 * g + 2] * correct, sum[k][4 * g + 3] * correct);
+    }
+}
+
 // A workgroup: query_groups (1, 2 or 4) x QT x 32 queries, a part of the rows, of which each of 4 / query_groups groups of waves
 // takes some tiles of every stage (and has a part of its own in `parts`), and COLUMNS columns.
 template <typename SHAPE, bool BIAS, bool ENTROPY, int COLUMNS, int QT>
@@ -146,7 +250,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   if (BIAS) next_bias = mx_bias(bias, next_row);
 
   MxRow<SHAPE> q[QT];
-  float q_lse[QT], base[QT], correct[QT], a[QT], b[QT];
+  MxGradQuery<BIAS> query[QT];
   MxTile sum[QT][BLOCKS];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -154,27 +258,12 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
     mx_load_row<SHAPE>(queries, mine, blocks, &q[t]);
     mx_clear_rest<SHAPE>(blocks, &q[t]);
     if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[t]);
-    // (-inf: all rows are out, and any number will do)
-    q_lse[t] = lse[mine] == -kMxInf ? 0.f : lse[mine];
-    // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p
-    base[t] = q_lse[t] * kMxLog2e;
-    const float rest = __fmaf_rn(q_lse[t], kMxLog2e, -base[t]) + q_lse[t] * 1.92596300e-8f;
-    correct[t] = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base[t], -rest));
-    if (ENTROPY) {
-      float u = 0.f;
-#pragma unroll 8
-      for (u32 g = half; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)mine * n_given + g, rows.n, bias);
-      u += __shfl_xor(u, 32, kWave);
-      const float h = d_entropy[mine];
-      a[t] = -__fmaf_rn(h, entropy[mine], u);
-      b[t] = -h * kMxLn2;
-    }
+    query[t].load(mine, unit, lse);
+    if (ENTROPY) query[t].load_entropy(mine, entropy, d_entropy, given, d_logp, n_given, rows.n, bias);
 #pragma unroll
     for (int k = 0; k < BLOCKS; ++k) sum[t][k] = mx_zero_tile();
   }
-  // (-1, 0) and (0, -1) in bfloat16, in registers: the second as a constant of the instruction is not what the GPU takes it for
-  u32 minus_low = 0x0000BF80u, minus_high = 0xBF800000u;
-  asm("" : "+v"(minus_low), "+v"(minus_high));
+  const MxOnes ones;
 
   unpack.store(first + wave * kMxTile, end, col0, row_bytes, s_rows[0][wave]);
   __syncthreads();
@@ -214,57 +303,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
       for (int t = 0; t < QT; ++t) d[t] = mx_products<SHAPE>(r, q[t], blocks);
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        float most = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = d[t][i];
-          const float log2_p = BIAS ? (__fmaf_rn(x, scale, x_bias[i]) - q_lse[t]) * unit.unit : __fmaf_rn(x, unit.unit, -base[t]);
-          const float p = exp2_fast(log2_p);
-          most = fmaxf(most, p);
-          // (log p of a row far below, or out, is not multiplied with: its p is 0)
-          d[t][i] = ENTROPY ? p * __fmaf_rn(b[t], BIAS ? fmaxf(log2_p, -200.f) : log2_p, a[t]) : p;
-        }
-        const bool all_pieces = __any(most > kMxLarge);
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
-          MxHalves8 value[BLOCKS];
-#pragma unroll
-          for (int k = 0; k < BLOCKS; ++k)
-            value[k] = *reinterpret_cast<const MxHalves8*>(&s_rows[buffer][tile][mx_unit(k, step, lane) * 2]);
-          auto add = [&](const u32* piece) {
-            const uint4 w = make_uint4(piece[0], piece[1], piece[2], piece[3]);
-#pragma unroll
-            for (int k = 0; k < BLOCKS; ++k)
-              sum[t][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[t][k], 0, 0, 0);
-          };
-          // pairs of rows: the upper halves of both; what they leave (c - 1 x piece in one instruction, exactly), rounded;
-          // and what that leaves
-          float c[8];
-          u32 piece[4];
-          auto take_off = [&] {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              const MxHalves2 both = __builtin_bit_cast(MxHalves2, piece[i / 2]);
-              c[i] = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(MxHalves2, minus_low), c[i], false);
-              c[i + 1] = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(MxHalves2, minus_high), c[i + 1], false);
-            }
-          };
-#pragma unroll
-          for (int i = 0; i < 8; ++i) c[i] = d[t][8 * step + i];
-#pragma unroll
-          for (int i = 0; i < 8; i += 2) piece[i / 2] = __builtin_amdgcn_perm(__float_as_uint(c[i + 1]), __float_as_uint(c[i]), 0x07060302u);
-          add(piece);
-          take_off();
-#pragma unroll
-          for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
-          add(piece);
-          if (all_pieces) {
-            take_off();
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
-            add(piece);
-          }
-        }
+        mx_add_tile<BIAS, ENTROPY, BLOCKS>(d[t], x_bias, scale, query[t], unit.unit, s_rows[buffer][tile], ones, sum[t]);
       }
     }
     unpack.store(stage0 + kMxStageRows + wave * kMxTile, end, col0, row_bytes, s_rows[buffer ^ 1u][wave]);
@@ -272,19 +311,90 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const u32 query = query0 + t * kMxTile;
-    if (query >= queries.n) continue;
-    float* to = parts + ((u64)(blockIdx.x * splits + split) * queries.n + query) * dim;
-#pragma unroll
-    for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const u32 col = col0 + k * 32 + 8 * g + 4 * half;
-        if (col < dim)
-          *reinterpret_cast<float4*>(to + col) = make_float4(sum[t][k][4 * g] * correct[t], sum[t][k][4 * g + 1] * correct[t],
-                                                             sum[t][k][4 * g + 2] * correct[t], sum[t][k][4 * g + 3] * correct[t]);
-      }
+    const u32 mine = query0 + t * kMxTile;
+    if (mine < queries.n)
+      mx_store_sums<BLOCKS>(sum[t], query[t].correct, col0, dim, parts + ((u64)(blockIdx.x * splits + split) * queries.n + mine) * dim);
   }
+}
+
+// Wide rows and more than a few queries: the four waves hold 32 queries each and go through the rows together, a tile in LDS for the
+// products and the next two tiles' columns unpacked (by two waves a tile).
+template <typename SHAPE, bool BIAS, bool ENTROPY>
+__global__ void __launch_bounds__(kMxThreads) HPS_MX_WAVES
+mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, MxGradUnit unit, const float* __restrict__ bias,
+                   const float* __restrict__ lse, const float* __restrict__ entropy, const i32* __restrict__ given,
+                   const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ d_entropy, u32 part_rows, float* __restrict__ parts) {
+  constexpr u32 COLUMNS = 128, BLOCKS = COLUMNS / 32, kStage = 2;
+  constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;
+  typedef MxShared<SHAPE> Shared;
+  __shared__ int4 s_tile[2][Shared::UNITS];
+  __shared__ uint2 s_rows[2][kStage][kTileWords];
+  __shared__ float s_bias[2][kMxTile];
+  const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const u32 mine = (blockIdx.y * (kMxThreads / kWave) + wave) * kMxTile + lane % 32;
+  const u32 first = blockIdx.x * part_rows, end = min(rows.n - first, part_rows) + first, col0 = blockIdx.z * COLUMNS;
+  const u32 my_tile = wave / 2 * kMxTile, my_col = col0 + wave % 2 * (COLUMNS / 2), my_words = wave % 2 * (kTileWords / 2);
+
+  MxUnpack<COLUMNS / 2, BIAS> unpack;
+  unpack.load(rows, first + my_tile, my_col, row_bytes, blocks, bias);
+  int4 own[Shared::OWN];
+  u32 scales[SHAPE::SCALE_WORDS];
+  float my_bias = 0.f;
+  Shared::load(rows, first, blocks, own);
+  mx_load_scales<SHAPE>(rows, min(first + lane % 32, rows.n - 1), blocks, scales);
+  if (BIAS) my_bias = mx_bias(bias, min(first + lane % 32, rows.n - 1));
+  MxRow<SHAPE> q;
+  MxGradQuery<BIAS> query;
+  MxTile sum[BLOCKS];
+  mx_load_row<SHAPE>(queries, min(mine, queries.n - 1), blocks, &q);
+  mx_clear_rest<SHAPE>(blocks, &q);
+  if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
+  query.load(min(mine, queries.n - 1), unit, lse);
+  if (ENTROPY) query.load_entropy(min(mine, queries.n - 1), entropy, d_entropy, given, d_logp, n_given, rows.n, bias);
+#pragma unroll
+  for (u32 k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();
+  const MxOnes ones;
+
+  unpack.store(first + my_tile, end, my_col, row_bytes, s_rows[0][wave / 2] + my_words);
+  u32 buffer = 0, tile_buffer = 0;
+  for (u32 stage0 = first; stage0 < end; stage0 += kStage * kMxTile, buffer ^= 1u) {
+    for (u32 tile = 0; tile < kStage; ++tile, tile_buffer ^= 1u) {
+      const u32 row0 = stage0 + tile * kMxTile;
+      Shared::store(own, blocks, s_tile[tile_buffer]);
+      u32 r_scales[SHAPE::SCALE_WORDS];
+#pragma unroll
+      for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r_scales[w] = scales[w];
+      if (BIAS) {
+        const float b = row0 + lane % 32 < end ? my_bias : -kMxInf;
+        if (b == -kMxInf) {
+#pragma unroll
+          for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r_scales[w] = 0;
+        }
+        if (threadIdx.x < kMxTile) s_bias[tile_buffer][lane] = b;
+      }
+      // (what is written before this barrier was last read before the one before it)
+      __syncthreads();
+      const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
+      Shared::load(rows, row0 + kMxTile, blocks, own);
+      mx_load_scales<SHAPE>(rows, ahead, blocks, scales);
+      if (BIAS) my_bias = mx_bias(bias, ahead);
+      if (tile == 0) unpack.load(rows, stage0 + kStage * kMxTile + my_tile, my_col, row_bytes, blocks, bias);
+      __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)
+      if (row0 >= end) continue;
+      float x_bias[16];
+      if (BIAS) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 v = *reinterpret_cast<const float4*>(&s_bias[tile_buffer][8 * g + 4 * half]);
+          x_bias[4 * g] = v.x; x_bias[4 * g + 1] = v.y; x_bias[4 * g + 2] = v.z; x_bias[4 * g + 3] = v.w;
+        }
+      }
+      const MxTile d = mx_products_shared<SHAPE>(s_tile[tile_buffer], r_scales, q, blocks);
+      mx_add_tile<BIAS, ENTROPY, (int)BLOCKS>(d, x_bias, scale, query, unit.unit, s_rows[buffer][tile], ones, sum);
+    }
+    unpack.store(stage0 + kStage * kMxTile + my_tile, end, my_col, row_bytes, s_rows[buffer ^ 1u][wave / 2] + my_words);
+  }
+  if (mine < queries.n) mx_store_sums<(int)BLOCKS>(sum, query.correct, col0, dim, parts + ((u64)blockIdx.x * queries.n + mine) * dim);
 }
 
 // The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.
