@@ -397,26 +397,27 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
   if (mine < queries.n) mx_store_sums<(int)BLOCKS>(sum, query.correct, col0, dim, parts + ((u64)blockIdx.x * queries.n + mine) * dim);
 }
 
-// The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.
+// The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.  Added up in 64 bits: the two
+// may cancel almost entirely.
 constexpr u32 kMxEndWaves = 16;
 template <bool BIAS, bool ENTROPY>
 __global__ void __launch_bounds__(kMxEndWaves * kWave)
 mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, float scale, const float* __restrict__ bias,
                 const i32* __restrict__ given, const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ parts,
                 u32 n_parts, float* __restrict__ out) {
-  __shared__ float s_sum[kMxEndWaves][kWave], s_given[kMxEndWaves][kWave], s_u[kMxEndWaves][kWave];
+  __shared__ double s_sum[kMxEndWaves][kWave], s_given[kMxEndWaves][kWave], s_u[kMxEndWaves][kWave];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave;
   const u64 total = (u64)n_queries * dim, i = (u64)blockIdx.x * kWave + lane;
   if (i < total) {
     const u32 query = (u32)(i / dim), col = (u32)(i - (u64)query * dim);
-    float sum = 0.f, of_given = 0.f, u_all = 0.f;
+    double sum = 0.0, of_given = 0.0, u_all = 0.0;
 #pragma unroll 8
     for (u32 p = wave; p < n_parts; p += kMxEndWaves) sum += parts[p * total + i];
     for (u32 g = wave; g < n_given; g += kMxEndWaves) {
       const u64 at = (u64)query * n_given + g;
       const float u = mx_upstream<BIAS>(given, d_logp, at, rows.n, bias);
       u_all += u;
-      if (u != 0.f) of_given += u * mx_value(rows, (u32)given[at], col, row_bytes, blocks);
+      if (u != 0.f) of_given += (double)u * mx_value(rows, (u32)given[at], col, row_bytes, blocks);
     }
     s_sum[wave][lane] = sum;
     s_given[wave][lane] = of_given;
@@ -424,14 +425,14 @@ mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, 
   }
   __syncthreads();
   if (wave == 0 && i < total) {
-    float sum = 0.f, of_given = 0.f, u_all = 0.f;
+    double sum = 0.0, of_given = 0.0, u_all = 0.0;
 #pragma unroll
     for (u32 w = 0; w < kMxEndWaves; ++w) {
       sum += s_sum[w][lane];
       of_given += s_given[w][lane];
       u_all += s_u[w][lane];
     }
-    out[i] = scale * ((ENTROPY ? sum : -u_all * sum) + of_given);
+    out[i] = (float)(scale * ((ENTROPY ? sum : -u_all * sum) + of_given));
   }
 }
 

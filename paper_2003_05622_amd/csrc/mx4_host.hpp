@@ -109,7 +109,7 @@ hps_status hps_mx4_quantize(const void* d_values, hps_value_type type, uint64_t 
 }
 
 hps_status hps_mx4_dequantize(const hps_mx4_rows* rows, uint32_t dim, float* d_out, void* stream) {
-  if (!mx_dim_ok(dim) || !mx_rows_ok(rows, dim, 1ull << 30)) return HPS_EINVAL;
+  if (!mx_dim_ok(dim) || !mx_rows_ok(rows, dim, (1ull << 40) / dim)) return HPS_EINVAL;
   if (rows->n == 0) return HPS_OK;
   if (!d_out || !mx_aligned(d_out, 16)) return HPS_EINVAL;
   mx_dequantize<<<grid_for(rows->n * mx_ceil(dim, 8), kMxThreads, 1u << 20), kMxThreads, 0, static_cast<hipStream_t>(stream)>>>(

@@ -543,3 +543,81 @@ def test_a_run_of_them_together(dim):
             acc = float(a0[at[0], 0]) + np.mean(g * g)
             w = w0[at[0]].double().cpu().numpy() - 0.05 * g / (np.sqrt(acc) + 1e-8)
             assert np.all(np.abs(w1[at[0]] - w) <= 1e-6 + 1e-5 * np.abs(w))
+
+
+# ---- large ones ----------------------------------------------------------------------------------
+def test_a_catalogue_beyond_32_bits():
+    """Codes of more than 2^32 bytes: the rows on both sides of that offset, and the last ones, count like any others."""
+    n, dim, m = (1 << 27) + 5003, 64, 3
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    codes = torch.randint(-2 ** 63, 2 ** 63 - 1, (n, 4), generator=gen, device="cuda").view(torch.uint8)
+    r = hps.Mx4Rows(codes, torch.full((n, 2), 120, dtype=torch.uint8, device="cuda"), dim)
+    q, _ = make(np.random.default_rng(3), m, dim)
+    # copies of the queries, larger than anything else, where offsets pass 2^31 and 2^32 bytes and at the end
+    spots = [0, (1 << 26) - 1, 1 << 26, (1 << 27) - 1, 1 << 27, n - 1]
+    for k, at in enumerate(spots):
+        r.codes[at] = q.codes[k % m]
+        r.scales[at] = 135
+    out = hps.mx4_scores(q, r, 0.01)
+    for first, last in ((0, 300), ((1 << 26) - 200, (1 << 26) + 200), ((1 << 27) - 200, (1 << 27) + 200), (n - 333, n)):
+        assert torch.equal(out[:, first:last], hps.mx4_scores(q, r[first:last], 0.01))
+    given = dev(np.array([[spots[k], spots[k + 3]] for k in range(m)], dtype=np.int32))
+    got = hps.mx4_logprobs(q, r, given, 10, 0.01)
+    best = torch.topk(out, 12, dim=1)
+    assert torch.equal(got.top_index[:, :2].long().sort().values, best.indices[:, :2].sort().values)
+    lse = torch.logsumexp(out.double(), 1)
+    assert (got.lse.double() - lse).abs().max() <= 1e-5 * lse.abs().max()
+    assert (got.logp.double() - (out.gather(1, given.long()).double() - lse[:, None])).abs().max() <= 1e-4
+    u = torch.full((m, 2), -0.5, device="cuda")
+    # nearly all of the probability lies on the copies: the gradient is that of a catalogue of these alone, as far as they count
+    d = hps.mx4_logprobs_backward(q, r, given, u, got.lse, scale=0.01)
+    p = torch.exp(out.double() - lse[:, None])
+    assert p[:, spots].sum(1).min() > 0.999
+    w = hps.Mx4Rows(r.codes[spots].contiguous(), r.scales[spots].contiguous(), dim).dequantize().double()
+    at = {s: i for i, s in enumerate(spots)}
+    picked = torch.stack([w[[at[int(g)] for g in row]].sum(0) for row in given.cpu()]) * -0.5
+    want = 0.01 * (picked + p[:, spots] @ w)
+    size = 0.01 * w.abs().max()
+    assert (d.double() - want).abs().max() <= 2e-3 * size       # (1 - 0.999 of a row's largest value, twice)
+    del out, codes, r
+    torch.cuda.empty_cache()
+
+
+def test_scores_beyond_32_bits():
+    m, n, dim = 70_000, 65_540, 4
+    (q, _), (r, _) = make(np.random.default_rng(4), m, dim), make(np.random.default_rng(5), n, dim)
+    out = hps.mx4_scores(q, r, dtype=torch.bfloat16)
+    for a, b in ((0, 40), (32_760, 32_780), (65_520, 65_560), (m - 33, m)):
+        assert torch.equal(out[a:b], hps.mx4_scores(q[a:b], r, dtype=torch.bfloat16))
+    del out
+    torch.cuda.empty_cache()
+
+
+def test_rows_of_a_table_beyond_32_bits_of_codes():
+    """A strided input whose rows start more than 2^32 bytes in."""
+    n, dim, wide = 1 << 21, 32, 1024
+    x = torch.empty((n, wide), dtype=torch.bfloat16, device="cuda")
+    x[:, :dim] = torch.randn((n, dim), device="cuda")
+    rows = hps.mx4_quantize(x[:, :dim])
+    for a, b in ((0, 100), ((1 << 21) - 100, 1 << 21), ((1 << 20) - 50, (1 << 20) + 50)):
+        want = hps.mx4_quantize(x[a:b, :dim].contiguous())
+        assert torch.equal(rows.codes[a:b], want.codes) and torch.equal(rows.scales[a:b], want.scales)
+
+
+@pytest.mark.parametrize("m,n,dim", [(1, 1, 8), (300, 7, 16), (1500, 1, 64), (2000, 33, 1024), (5, 100_000, 1024), (70, 3000, 1000)])
+def test_extreme_shapes(m, n, dim):
+    rng = np.random.default_rng(m + n)
+    (q, qv), (r, rv) = make(rng, m, dim), make(rng, n, dim, 0.1)
+    given = rng.integers(0, n, size=(m, 2)).astype(np.int32)
+    check_logprobs(q, qv, r, rv, 10 / np.sqrt(dim), None, given, 5)
+    check_gradient(q, qv, r, rv, 10 / np.sqrt(dim), None, given, rng.normal(size=(m, 2)).astype(np.float32), rng.normal(size=m).astype(np.float32))
+
+
+def test_an_entropy_that_is_all_there_is_to_lose():
+    """Few rows, many given ones: terms that cancel almost entirely."""
+    rng = np.random.default_rng(11)
+    for seed in range(20):
+        (q, qv), (r, rv) = make(rng, 2, 64), make(rng, 3, 64, 0.1)
+        given = rng.integers(-1, 3, size=(2, 16)).astype(np.int32)
+        check_gradient(q, qv, r, rv, 0.6, None, given, (0.1 * rng.normal(size=(2, 16))).astype(np.float32), rng.normal(size=2).astype(np.float32))
