@@ -21,20 +21,40 @@ constexpr u32 kMxNoScale = 255;       // the scale byte of a block that stands f
 __host__ __device__ constexpr u32 mx_row_bytes(u32 dim) { return dim <= 8 ? 4u : dim <= 16 ? 8u : (dim + kMxBlock - 1) / kMxBlock * 16; }
 __host__ __device__ constexpr u32 mx_blocks(u32 dim) { return (dim + kMxBlock - 1) / kMxBlock; }
 
-// Eight values of a block's lane group: the group of GL lanes (4; narrow rows: 1 or 2) holds a whole block.
+// The value of lane l ^ D, by moves between lanes (a shuffle goes through the LDS and takes some hundred cycles).
+template <int D>
+__device__ __forceinline__ u32 mx_lane_xor(u32 v) {
+  static_assert(D == 1 || D == 2 || D == 4 || D == 8 || D == 16 || D == 32, "");
+  if constexpr (D == 1) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);
+  if constexpr (D == 2) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);
+  // (the lanes of eight, and then of each four, backwards)
+  if constexpr (D == 4) return (u32)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
+  if constexpr (D == 8) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);
+  if constexpr (D == 16) {
+    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane_id() & 16u ? both[0] : both[1];
+  }
+  if constexpr (D == 32) {
+    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane_id() & 32u ? both[0] : both[1];
+  }
+}
+
+// Some of a block's values: a group of lanes with four or eight of them each holds a whole block.
 struct MxEight {
   float v[8];
   __device__ __forceinline__ void set(int q, float4 f) { v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w; }
 };
 
-// The scale byte of the block whose values the lane group holds, and the lane's eight codes.
-template <int GL>
+// The scale byte of the block whose values GL lanes hold, VALUES each, and the lane's codes.
+template <int GL, int VALUES = 8>
 __device__ __forceinline__ u32 mx_encode(const MxEight& x, u32* codes) {
   u32 most = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x.v[i]) & 0x7FFFFFFFu);
-#pragma unroll
-  for (int d = 1; d < GL; d *= 2) most = max(most, (u32)__shfl_xor((int)most, d, kWave));
+  for (int i = 0; i < VALUES; ++i) most = max(most, __float_as_uint(x.v[i]) & 0x7FFFFFFFu);
+  if (GL > 1) most = max(most, mx_lane_xor<1>(most));
+  if (GL > 2) most = max(most, mx_lane_xor<2>(most));
+  if (GL > 4) most = max(most, mx_lane_xor<4>(most));
   const u32 e = most >> 23;
   if (e == 255) {
     *codes = 0;
@@ -46,8 +66,10 @@ __device__ __forceinline__ u32 mx_encode(const MxEight& x, u32* codes) {
   u32 c = 0;
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[0], x.v[1], s, 0);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2], x.v[3], s, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[4], x.v[5], s, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[6], x.v[7], s, 3);
+  if (VALUES == 8) {
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[4], x.v[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[6], x.v[7], s, 3);
+  }
   *codes = c;
   return scale;
 }
@@ -80,16 +102,15 @@ __device__ __forceinline__ float4 load_values4(const void* base, u64 at) {
   return *reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
 }
 
-// One lane group per block, flat over all blocks.
+// Eight values a lane, GL lanes a block, flat over all blocks.  Bound by memory: 2^28 float32 values, 64 a row, in 208 us (1.2 GB).
 template <bool BF16, int GL>
 __global__ void __launch_bounds__(kMxThreads)
-mx_quantize(const void* __restrict__ values, u64 n, u32 dim, u64 stride, uint8_t* __restrict__ codes,
-            uint8_t* __restrict__ scales, float* __restrict__ rounded) {
-  const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
+mx_quantize(const void* __restrict__ values, u64 n, u32 dim, u64 stride, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim), sub = threadIdx.x % GL;
   const u64 total = n * blocks;
   for (u64 b = ((u64)blockIdx.x * kMxThreads + threadIdx.x) / GL; b < total; b += (u64)gridDim.x * (kMxThreads / GL)) {
-    const u64 row = b / blocks;
-    const u32 block = (u32)(b - row * blocks), sub = threadIdx.x % GL, col = block * kMxBlock + 8 * sub;
+    const u64 row = total < (1ull << 32) ? (u32)b / blocks : b / blocks;
+    const u32 block = (u32)(b - row * blocks), col = block * kMxBlock + 8 * sub;
     MxEight x;
 #pragma unroll
     for (int q = 0; q < 2; ++q)
@@ -98,28 +119,63 @@ mx_quantize(const void* __restrict__ values, u64 n, u32 dim, u64 stride, uint8_t
     const u32 scale = mx_encode<GL>(x, &c);
     *reinterpret_cast<u32*>(codes + row * row_bytes + block * 16 + 4 * sub) = c;
     if (sub == 0) scales[b] = (uint8_t)scale;
-    if (rounded) {
-      const MxEight y = mx_decode(c, scale);
+  }
+}
+
+// With the values that the codes stand for: four a lane, LANES (8; narrow rows: 2 or 4) lanes a block, so that a wave stores 1 KB in one piece
+// past the L2 (in pieces of 32 bytes a lane that takes 604 us for the 2.3 GB above, through it 399; so 394, and 292 from bfloat16
+// instead of 345; without the values the other form is faster, 208 us to 220); kMxInFlight turns are loaded before the first is worked on.
+constexpr int kMxInFlight = 4;
+template <bool BF16, int LANES>
+__global__ void __launch_bounds__(kMxThreads)
+mx_quantize_round(const void* __restrict__ values, u64 n, u32 dim, u64 stride, uint8_t* __restrict__ codes,
+                  uint8_t* __restrict__ scales, float* __restrict__ rounded) {
+  constexpr u32 kUnits = kMxThreads / LANES;                           // blocks a turn of the workgroup takes
+  const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim), sub = threadIdx.x % LANES;
+  const u64 total = n * blocks;
+  const u32 more_rows = kUnits / blocks, more_blocks = kUnits % blocks;
+  for (u64 b0 = (u64)blockIdx.x * (kMxInFlight * kUnits) + threadIdx.x / LANES; b0 < total; b0 += (u64)gridDim.x * (kMxInFlight * kUnits)) {
+    u64 row[kMxInFlight];
+    u32 col[kMxInFlight];
+    float4 v[kMxInFlight];
+    u64 at = total < (1ull << 32) ? (u32)b0 / blocks : b0 / blocks;    // (a division of 64 bits takes longer than all the rest)
+    u32 block = (u32)(b0 - at * blocks);
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
-        if (col + 4 * q < dim)
-          *reinterpret_cast<float4*>(rounded + row * dim + col + 4 * q) = make_float4(y.v[4 * q], y.v[4 * q + 1], y.v[4 * q + 2], y.v[4 * q + 3]);
+    for (int q = 0; q < kMxInFlight; ++q) {
+      row[q] = at;
+      col[q] = block * kMxBlock + 4 * sub;
+      v[q] = at < n && col[q] < dim ? load_values4<BF16>(values, at * stride + col[q]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      at += more_rows;
+      block += more_blocks;
+      if (block >= blocks) { block -= blocks; ++at; }
+    }
+#pragma unroll
+    for (int q = 0; q < kMxInFlight; ++q) {
+      if (row[q] >= n) break;
+      MxEight x = {};
+      x.set(0, v[q]);
+      u32 c;
+      const u32 scale = mx_encode<LANES, 4>(x, &c);
+      *reinterpret_cast<uint16_t*>(codes + row[q] * row_bytes + col[q] / 2) = (uint16_t)c;
+      if (sub == 0) scales[b0 + q * kUnits] = (uint8_t)scale;
+      if (col[q] < dim) {
+        const MxEight y = mx_decode(c, scale);
+        store_caller4(rounded + row[q] * dim + col[q], true, make_float4(y.v[0], y.v[1], y.v[2], y.v[3]));
+      }
     }
   }
 }
 
-// Eight values a lane.
+// Four values a lane, so that a wave stores 1 KB in one piece.
 __global__ void __launch_bounds__(kMxThreads)
 mx_dequantize(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, u64 n, u32 dim, float* __restrict__ out) {
-  const u32 words = (dim + 7) / 8, row_bytes = mx_row_bytes(dim), blocks = mx_blocks(dim);
+  const u32 words = dim / 4, row_bytes = mx_row_bytes(dim), blocks = mx_blocks(dim);
   const u64 total = n * words;
   for (u64 i = (u64)blockIdx.x * kMxThreads + threadIdx.x; i < total; i += (u64)gridDim.x * kMxThreads) {
     const u64 row = i / words;
     const u32 word = (u32)(i - row * words);
-    const MxEight y = mx_decode(*reinterpret_cast<const u32*>(codes + row * row_bytes + 4 * word), scales[row * blocks + word / 4]);
-    float* to = out + row * dim + 8 * word;
-    *reinterpret_cast<float4*>(to) = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
-    if (8 * word + 4 < dim) *reinterpret_cast<float4*>(to + 4) = make_float4(y.v[4], y.v[5], y.v[6], y.v[7]);
+    const MxEight y = mx_decode(*reinterpret_cast<const uint16_t*>(codes + row * row_bytes + 2 * word), scales[row * blocks + word / 8]);
+    store_caller4(out + 4 * i, true, make_float4(y.v[0], y.v[1], y.v[2], y.v[3]));
   }
 }
 

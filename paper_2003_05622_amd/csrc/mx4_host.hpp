@@ -99,10 +99,15 @@ hps_status hps_mx4_quantize(const void* d_values, hps_value_type type, uint64_t 
     return HPS_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
   mx_by_width(dim, [&](auto width) {
-    constexpr int GL = decltype(width)::value / 4;
-    const unsigned blocks = grid_for(n * mx_blocks(dim), kMxThreads / GL, 1u << 20);
+    constexpr int GL = decltype(width)::value / 4, LANES = 2 * GL;
+    const uint64_t all = n * mx_blocks(dim);
     mx_by_flag(type == HPS_VALUES_BF16, [&](auto bf16) {
-      mx_quantize<decltype(bf16)::value, GL><<<blocks, kMxThreads, 0, s>>>(d_values, n, dim, stride, d_codes, d_scales, d_rounded);
+      constexpr bool BF16 = decltype(bf16)::value;
+      if (d_rounded)
+        mx_quantize_round<BF16, LANES><<<grid_for(all, kMxThreads / LANES * kMxInFlight, 1u << 20), kMxThreads, 0, s>>>(
+            d_values, n, dim, stride, d_codes, d_scales, d_rounded);
+      else
+        mx_quantize<BF16, GL><<<grid_for(all, kMxThreads / GL, 1u << 20), kMxThreads, 0, s>>>(d_values, n, dim, stride, d_codes, d_scales);
     });
   });
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
@@ -112,7 +117,7 @@ hps_status hps_mx4_dequantize(const hps_mx4_rows* rows, uint32_t dim, float* d_o
   if (!mx_dim_ok(dim) || !mx_rows_ok(rows, dim, (1ull << 40) / dim)) return HPS_EINVAL;
   if (rows->n == 0) return HPS_OK;
   if (!d_out || !mx_aligned(d_out, 16)) return HPS_EINVAL;
-  mx_dequantize<<<grid_for(rows->n * mx_ceil(dim, 8), kMxThreads, 1u << 20), kMxThreads, 0, static_cast<hipStream_t>(stream)>>>(
+  mx_dequantize<<<grid_for(rows->n * (dim / 4), kMxThreads, 1u << 20), kMxThreads, 0, static_cast<hipStream_t>(stream)>>>(
       rows->d_codes, rows->d_scales, rows->n, dim, d_out);
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
 }

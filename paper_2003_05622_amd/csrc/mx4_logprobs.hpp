@@ -258,24 +258,6 @@ __device__ __forceinline__ float mx_candidate_score(u64 c) {
 }
 __device__ __forceinline__ u32 mx_candidate_number(u64 c) { return ~(u32)c; }
 
-// The value of lane l ^ D, by moves between lanes (a shuffle through the LDS takes some hundred cycles, and a sort has 21).
-template <int D>
-__device__ __forceinline__ u32 mx_lane_xor(u32 v) {
-  static_assert(D == 1 || D == 2 || D == 4 || D == 8 || D == 16 || D == 32, "");
-  if constexpr (D == 1) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);
-  if constexpr (D == 2) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);
-  // (the lanes of eight, and then of each four, backwards)
-  if constexpr (D == 4) return (u32)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
-  if constexpr (D == 8) return (u32)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);
-  if constexpr (D == 16) {
-    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return lane_id() & 16u ? both[0] : both[1];
-  }
-  if constexpr (D == 32) {
-    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return lane_id() & 32u ? both[0] : both[1];
-  }
-}
 template <int D>
 __device__ __forceinline__ u64 mx_exchange(u64 c, bool larger) {
   const u64 o = (u64)mx_lane_xor<D>((u32)(c >> 32)) << 32 | mx_lane_xor<D>((u32)c);
