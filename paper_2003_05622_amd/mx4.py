@@ -40,10 +40,9 @@ class Mx4Rows:
             raise ValueError("rows of dim %d: codes must be uint8 [n, %d] and scales uint8 [n, %d]" % ((dim,) + shape))
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("codes and scales must be contiguous")
-        device = codes.device
-        if device.type != "cuda" or scales.device != device:
+        if codes.get_device() < 0 or scales.get_device() != codes.get_device():
             raise ValueError("codes and scales must be on one GPU")
-        self.codes, self.scales, self.dim, self.n, self.device = codes, scales, dim, n, device
+        self.codes, self.scales, self.dim, self.n, self.device = codes, scales, dim, n, codes.device
 
     @classmethod
     def empty(cls, n: int, dim: int, device) -> "Mx4Rows":
@@ -105,7 +104,7 @@ def _array(t, name: str, dtype, shape, device):
     """Address of a contiguous tensor of this type, shape and GPU (None stays None)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device.index:
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
     return t.data_ptr()
 
