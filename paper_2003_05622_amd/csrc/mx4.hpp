@@ -243,8 +243,11 @@ struct MxShape {
   static constexpr int WIDTH = WIDTH_, STEPS = STEPS_;
   // whether the next rows are loaded while the present ones are worked on (wide rows fill the registers by themselves)
   static constexpr bool AHEAD = STEPS <= 4;
-  // words that hold the scale bytes of a lane's blocks, four to a word
-  static constexpr int SCALE_WORDS = (STEPS + 3) / 4;
+  // words that hold the scale bytes of a lane's blocks: one each, or of wide rows four to a word
+  static constexpr bool PACKED = STEPS > 4;
+  static constexpr int SCALE_WORDS = PACKED ? STEPS / 4 : STEPS;
+  // (a shape with half the steps would do for up to STEPS blocks: the first STEPS / 2 + 1 steps are always there)
+  static constexpr int SURE = STEPS / 2 + 1;
 };
 
 // One operand of all steps, as lane l holds it: of its row blocks l / 32, 2 + l / 32, ...
@@ -264,14 +267,24 @@ __device__ __forceinline__ int4 mx_load_block(const uint8_t* at) {
   return make_int4(*reinterpret_cast<const int*>(at), 0, 0, 0);
 }
 
+// The byte behind the last block of an odd number is another row's, and may stand for NaN.
+template <typename SHAPE>
+__device__ __forceinline__ void mx_clear_last_scale(u32 blocks, u32* scales) {
+  if (!(blocks & 1u)) return;
+#pragma unroll
+  for (int w = 0; w < SHAPE::SCALE_WORDS; ++w)
+    if (lane_id() >= 32 && blocks / 8 == (u32)w) scales[w] &= ~(0xFFu << (8 * (blocks / 2 % 4)));
+}
+
 // The scale bytes of a lane's blocks of row `row` (below n).  A block that the row does not have (`blocks` is odd, or below 2 *
 // STEPS - 1) has some scale, not that of a NaN unless the row has one.
 template <typename SHAPE>
 __device__ __forceinline__ void mx_load_scales(const MxHeld& m, u32 row, u32 blocks, u32* to) {
   const u32 half = lane_id() / 32;
   const u64 first = (u64)row * blocks;
-  if (SHAPE::STEPS == 1) {
-    to[0] = m.scales[first + min(half, blocks - 1)];
+  if (!SHAPE::PACKED) {
+#pragma unroll
+    for (int s = 0; s < SHAPE::STEPS; ++s) to[s] = m.scales[first + min(2 * s + half, blocks - 1)];
     return;
   }
   // Eight scale bytes at a time, those of four steps of both halves; where fewer are left in the array, the last
@@ -291,12 +304,7 @@ __device__ __forceinline__ void mx_load_scales(const MxHeld& m, u32 row, u32 blo
     }
     to[w] = __builtin_amdgcn_perm((u32)(eight >> 32), (u32)eight, half ? 0x07050301u : 0x06040200u);
   }
-  // (the byte behind the last block of an odd number is another row's, and may stand for NaN)
-  if (blocks & 1u) {
-#pragma unroll
-    for (int w = 0; w < SHAPE::SCALE_WORDS; ++w)
-      if (half && blocks / 8 == (u32)w) to[w] &= ~(0xFFu << (8 * (blocks / 2 % 4)));
-  }
+  mx_clear_last_scale<SHAPE>(blocks, to);
 }
 
 // Loads a lane's blocks of row `row` (below n).  A block that the row does not have is read as the row's last one: the
@@ -307,8 +315,33 @@ __device__ __forceinline__ void mx_load_row(const MxHeld& m, u32 row, u32 blocks
   const u64 first = (u64)row * blocks;
 #pragma unroll
   for (int s = 0; s < SHAPE::STEPS; ++s)
-    if (s == 0 || 2 * s < (int)blocks) to->codes[s] = mx_load_block<SHAPE::WIDTH>(m.codes + (first + min(2 * s + half, blocks - 1)) * SHAPE::WIDTH);
+    if (s < SHAPE::SURE || 2 * s < (int)blocks) to->codes[s] = mx_load_block<SHAPE::WIDTH>(m.codes + (first + min(2 * s + half, blocks - 1)) * SHAPE::WIDTH);
   mx_load_scales<SHAPE>(m, row, blocks, to->scales);
+}
+
+// The same for 32 neighbouring rows, lane l % 32 the row row0 + l % 32 (the last one where there is none), row0 the same in all lanes:
+// a scalar base and small offsets (a product of full width takes as long as four other instructions), and no branch, as
+// the loads of a loop are only waited for one by one if every turn has the same ones.
+struct MxTileRows {
+  u32 first, row;        // of the array, and of the lane from there
+  __device__ __forceinline__ MxTileRows(u32 n, u32 row0, u32 lane) {
+    first = min(row0, n - 1);
+    row = min(lane, n - 1 - first);
+  }
+};
+template <typename SHAPE>
+__device__ __forceinline__ void mx_load_tile(const MxHeld& m, u32 row0, u32 blocks, MxRow<SHAPE>* to) {
+  const u32 half = lane_id() / 32;
+  const MxTileRows at(m.n, row0, lane_id() % 32);
+  const uint8_t *codes = m.codes + (u64)at.first * blocks * SHAPE::WIDTH, *scales = m.scales + (u64)at.first * blocks;
+  const u32 first = __umul24(at.row, blocks);
+#pragma unroll
+  for (int s = 0; s < SHAPE::STEPS; ++s) {
+    const u32 block = first + min(2 * s + half, blocks - 1);
+    if (!SHAPE::PACKED || s < SHAPE::SURE || 2 * s < (int)blocks) to->codes[s] = mx_load_block<SHAPE::WIDTH>(codes + block * SHAPE::WIDTH);
+    if (!SHAPE::PACKED) to->scales[s] = scales[block];
+  }
+  if (SHAPE::PACKED) mx_load_scales<SHAPE>(m, at.first + at.row, blocks, to->scales);
 }
 
 // Takes out of an operand what mx_load_row has read in place of blocks that the rows do not have.
@@ -330,17 +363,18 @@ __device__ __forceinline__ void mx_negate(MxRow<SHAPE>* row) {
   }
 }
 
-template <int STEP>
+template <int BYTE>
 __device__ __forceinline__ MxTile mx_step(int4 a, u32 a_scales, int4 b, u32 b_scales, MxTile d) {
   constexpr int kFp4 = 4;
   const MxOperand wa = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, wb = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, wb, d, kFp4, kFp4, STEP % 4, (int)a_scales, STEP % 4, (int)b_scales);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, wb, d, kFp4, kFp4, BYTE, (int)a_scales, BYTE, (int)b_scales);
 }
 
 template <typename SHAPE, int STEP = 0>
 __device__ __forceinline__ void mx_steps(const MxRow<SHAPE>& a, const MxRow<SHAPE>& b, u32 blocks, MxTile* d) {
   if constexpr (STEP < SHAPE::STEPS) {
-    if (STEP == 0 || 2 * STEP < (int)blocks) *d = mx_step<STEP>(a.codes[STEP], a.scales[STEP / 4], b.codes[STEP], b.scales[STEP / 4], *d);
+    constexpr int WORD = SHAPE::PACKED ? STEP / 4 : STEP, BYTE = SHAPE::PACKED ? STEP % 4 : 0;
+    if (STEP < SHAPE::SURE || 2 * STEP < (int)blocks) *d = mx_step<BYTE>(a.codes[STEP], a.scales[WORD], b.codes[STEP], b.scales[WORD], *d);
     mx_steps<SHAPE, STEP + 1>(a, b, blocks, d);
   }
 }
@@ -388,8 +422,8 @@ struct MxShared {
 template <typename SHAPE, int STEP = 0>
 __device__ __forceinline__ void mx_steps_shared(const int4* tile, const u32* scales, const MxRow<SHAPE>& b, u32 blocks, MxTile* d) {
   if constexpr (STEP < SHAPE::STEPS) {
-    if (STEP == 0 || 2 * STEP < (int)blocks)
-      *d = mx_step<STEP>(MxShared<SHAPE>::get(tile, STEP), scales[STEP / 4], b.codes[STEP], b.scales[STEP / 4], *d);
+    if (STEP < SHAPE::SURE || 2 * STEP < (int)blocks)
+      *d = mx_step<STEP % 4>(MxShared<SHAPE>::get(tile, STEP), scales[STEP / 4], b.codes[STEP], b.scales[STEP / 4], *d);
     mx_steps_shared<SHAPE, STEP + 1>(tile, scales, b, blocks, d);
   }
 }

@@ -69,12 +69,14 @@ struct MxUnpack {
       place(p, &quad, &word);
       // (what is not there is read elsewhere, and left out when it is stored)
       const u32 byte = min((col0 + 8 * word) / 2, row_bytes - 4), block = min((col0 + 8 * word) / kMxBlock, blocks - 1);
+      const u32 first = min(row0, rows.n - 1);
+      const uint8_t *c = rows.codes + (u64)first * row_bytes, *s = rows.scales + (u64)first * blocks;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32 row = min(row0 + 4 * quad + i, rows.n - 1);
-        codes[p][i] = *reinterpret_cast<const u32*>(rows.codes + (u64)row * row_bytes + byte);
-        scales[p][i] = rows.scales[(u64)row * blocks + block];
-        if (BIAS) bias[p][i] = mx_bias(of_rows, row);
+        const u32 row = min(4 * quad + i, rows.n - 1 - first);
+        codes[p][i] = *reinterpret_cast<const u32*>(c + (__umul24(row, row_bytes) + byte));
+        scales[p][i] = s[__umul24(row, blocks) + block];
+        if (BIAS) bias[p][i] = mx_bias(of_rows + first, row);
       }
     }
   }
@@ -245,9 +247,8 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   unpack.load(rows, first + wave * kMxTile, col0, row_bytes, blocks, bias);
   MxRow<SHAPE> next;
   float next_bias = 0.f;
-  u32 next_row = min(first + split * kMxTile + lane % 32, rows.n - 1);
-  if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
-  if (BIAS) next_bias = mx_bias(bias, next_row);
+  if (SHAPE::AHEAD) mx_load_tile<SHAPE>(rows, first + split * kMxTile, blocks, &next);
+  if (BIAS) next_bias = mx_bias(bias, min(first + split * kMxTile + lane % 32, rows.n - 1));
 
   MxRow<SHAPE> q[QT];
   MxGradQuery<BIAS> query[QT];
@@ -275,12 +276,11 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
       if (row0 >= end) continue;
       MxRow<SHAPE> r;
       if (SHAPE::AHEAD) r = next;
-      else mx_load_row<SHAPE>(rows, min(row0 + lane % 32, rows.n - 1), blocks, &r);
+      else mx_load_tile<SHAPE>(rows, row0, blocks, &r);
       const float my_bias = row0 + lane % 32 < end ? next_bias : -kMxInf;
       const u32 ahead = tile + splits < kMxStageTiles ? row0 + splits * kMxTile : stage0 + kMxStageRows + split * kMxTile;
-      next_row = min(ahead + lane % 32, rows.n - 1);
-      if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, next_row, blocks, &next);
-      if (BIAS) next_bias = mx_bias(bias, next_row);
+      if (SHAPE::AHEAD) mx_load_tile<SHAPE>(rows, ahead, blocks, &next);
+      if (BIAS) next_bias = mx_bias(bias, min(ahead + lane % 32, rows.n - 1));
       __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)
       float x_bias[16];
       if (BIAS) {
@@ -376,7 +376,7 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
       __syncthreads();
       const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
       Shared::load(rows, row0 + kMxTile, blocks, own);
-      mx_load_scales<SHAPE>(rows, ahead, blocks, scales);
+      mx_load_scales<SHAPE>(rows, min(row0 + kMxTile + lane % 32, rows.n - 1), blocks, scales);
       if (BIAS) my_bias = mx_bias(bias, ahead);
       if (tile == 0) unpack.load(rows, stage0 + kStage * kMxTile + my_tile, my_col, row_bytes, blocks, bias);
       __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)

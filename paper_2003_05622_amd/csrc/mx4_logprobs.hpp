@@ -118,16 +118,16 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
   }
   MxRow<SHAPE> next;
   float next_bias = 0.f;
-  if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, min(first + lane % 32, rows.n - 1), blocks, &next);
+  if (SHAPE::AHEAD) mx_load_tile<SHAPE>(rows, first, blocks, &next);
   if (BIAS) next_bias = mx_bias(bias, min(first + lane % 32, rows.n - 1));
   u32 in_group = 0;
   for (u32 row0 = first; row0 < end; row0 += kMxTile) {
     MxRow<SHAPE> r;
     if (SHAPE::AHEAD) r = next;
-    else mx_load_row<SHAPE>(rows, min(row0 + lane % 32, rows.n - 1), blocks, &r);
+    else mx_load_tile<SHAPE>(rows, row0, blocks, &r);
     const float my_bias = row0 + lane % 32 < end ? next_bias : -kMxInf;
     const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
-    if (SHAPE::AHEAD) mx_load_row<SHAPE>(rows, ahead, blocks, &next);
+    if (SHAPE::AHEAD) mx_load_tile<SHAPE>(rows, row0 + kMxTile, blocks, &next);
     float b[16] = {};
     if (BIAS) {
       next_bias = mx_bias(bias, ahead);
@@ -219,7 +219,7 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
     __syncthreads();
     const u32 ahead = min(row0 + kMxTile + lane % 32, rows.n - 1);
     Shared::load(rows, row0 + kMxTile, blocks, own);
-    mx_load_scales<SHAPE>(rows, ahead, blocks, scales);
+    mx_load_scales<SHAPE>(rows, min(row0 + kMxTile + lane % 32, rows.n - 1), blocks, scales);
     if (BIAS) my_bias = mx_bias(bias, ahead);
     __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)
     float b[16] = {};

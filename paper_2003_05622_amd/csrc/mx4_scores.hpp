@@ -125,10 +125,10 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
     }
   } else {
     MxRow<SHAPE> next;
-    mx_load_row<SHAPE>(queries, min(begin * kMxTile + lane % 32, queries.n - 1), blocks, &next);
+    mx_load_tile<SHAPE>(queries, begin * kMxTile, blocks, &next);
     for (u32 tile = begin; tile < last; ++tile) {
       const MxRow<SHAPE> q = next;
-      mx_load_row<SHAPE>(queries, min((tile + 1) * kMxTile + lane % 32, queries.n - 1), blocks, &next);
+      mx_load_tile<SHAPE>(queries, (tile + 1) * kMxTile, blocks, &next);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < RT; ++t) d[t] = mx_products<SHAPE>(q, r[t], blocks);
