@@ -5,8 +5,8 @@
  *              nothing is allocated, calls enqueue work on `stream` and return, the GPU that
  *              holds the buffers is the current one.  Apart from hps_mx4_get these calls touch
  *              no table; any number of them may run at once, on any streams, as long as their
- *              outputs and workspaces are different buffers.  All of them may be captured into
- *              a HIP graph and replayed.
+ *              outputs and workspaces are different buffers.  No output may overlap an
+ *              input.  All of them may be captured into a HIP graph and replayed.
  *
  * What it is for: a trainer's rows (a catalogue of items or ads) are frozen for serving, an
  * eighth of their float32 size; pooled rows become queries; a request asks for the best rows of
@@ -104,7 +104,7 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
 /* The gradient of sum(d_dlogp * logp) + sum(d_dentropy * entropy) with respect to the values that the
  * queries' codes stand for: d_dqueries [queries, dim] float32, 16-byte aligned.
  *   d_lse, d_entropy  what hps_mx4_logprobs gave for the same arguments (d_entropy may be NULL if
- *                     d_dentropy is)
+ *                     d_dentropy is; with it the probabilities are a little more exact)
  *   d_given, d_dlogp  [queries, n_given] (both NULL: n_given 0); a row given twice counts twice; where d_given is no
  *                     row's number, or one of a row that is taken out, d_dlogp is not used
  *   d_dentropy        [queries] or NULL

@@ -127,13 +127,15 @@ struct MxGradUnit {
 template <bool BIAS>
 struct MxGradQuery {
   float lse, base, correct, a, b;
-  // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p
-  __device__ __forceinline__ void load(u32 query, const MxGradUnit& unit, const float* of_lse) {
+  // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p, and so, nearly, is
+  // what unit leaves: x unit is lse - entropy on average.
+  __device__ __forceinline__ void load(u32 query, const MxGradUnit& unit, const float* of_lse, const float* of_entropy) {
     // (-inf: all rows are out, and any number will do)
     lse = of_lse[query] == -kMxInf ? 0.f : of_lse[query];
     base = lse * kMxLog2e;
     const float rest = __fmaf_rn(lse, kMxLog2e, -base) + lse * 1.92596300e-8f;
-    correct = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, base, -rest));
+    const float x_unit = of_entropy ? base - of_entropy[query] * kMxLog2e : 0.f;
+    correct = BIAS ? 1.f : exp2f(__fmaf_rn(unit.off, x_unit, -rest));
     a = 1.f;
     b = 0.f;
   }
@@ -259,7 +261,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
     mx_load_row<SHAPE>(queries, mine, blocks, &q[t]);
     mx_clear_rest<SHAPE>(blocks, &q[t]);
     if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[t]);
-    query[t].load(mine, unit, lse);
+    query[t].load(mine, unit, lse, entropy);
     if (ENTROPY) query[t].load_entropy(mine, entropy, d_entropy, given, d_logp, n_given, rows.n, bias);
 #pragma unroll
     for (int k = 0; k < BLOCKS; ++k) sum[t][k] = mx_zero_tile();
@@ -349,7 +351,7 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
   mx_load_row<SHAPE>(queries, min(mine, queries.n - 1), blocks, &q);
   mx_clear_rest<SHAPE>(blocks, &q);
   if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
-  query.load(min(mine, queries.n - 1), unit, lse);
+  query.load(min(mine, queries.n - 1), unit, lse, entropy);
   if (ENTROPY) query.load_entropy(min(mine, queries.n - 1), entropy, d_entropy, given, d_logp, n_given, rows.n, bias);
 #pragma unroll
   for (u32 k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();
@@ -407,32 +409,36 @@ mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, 
                 u32 n_parts, float* __restrict__ out) {
   __shared__ double s_sum[kMxEndWaves][kWave], s_given[kMxEndWaves][kWave], s_u[kMxEndWaves][kWave];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave;
-  const u64 total = (u64)n_queries * dim, i = (u64)blockIdx.x * kWave + lane;
-  if (i < total) {
-    const u32 query = (u32)(i / dim), col = (u32)(i - (u64)query * dim);
-    double sum = 0.0, of_given = 0.0, u_all = 0.0;
+  const u64 total = (u64)n_queries * dim;
+  for (u64 i0 = (u64)blockIdx.x * kWave; i0 < total; i0 += (u64)gridDim.x * kWave) {
+    const u64 i = i0 + lane;
+    if (i < total) {
+      const u32 query = (u32)(i / dim), col = (u32)(i - (u64)query * dim);
+      double sum = 0.0, of_given = 0.0, u_all = 0.0;
 #pragma unroll 8
-    for (u32 p = wave; p < n_parts; p += kMxEndWaves) sum += parts[p * total + i];
-    for (u32 g = wave; g < n_given; g += kMxEndWaves) {
-      const u64 at = (u64)query * n_given + g;
-      const float u = mx_upstream<BIAS>(given, d_logp, at, rows.n, bias);
-      u_all += u;
-      if (u != 0.f) of_given += (double)u * mx_value(rows, (u32)given[at], col, row_bytes, blocks);
+      for (u32 p = wave; p < n_parts; p += kMxEndWaves) sum += parts[p * total + i];
+      for (u32 g = wave; g < n_given; g += kMxEndWaves) {
+        const u64 at = (u64)query * n_given + g;
+        const float u = mx_upstream<BIAS>(given, d_logp, at, rows.n, bias);
+        u_all += u;
+        if (u != 0.f) of_given += (double)u * mx_value(rows, (u32)given[at], col, row_bytes, blocks);
+      }
+      s_sum[wave][lane] = sum;
+      s_given[wave][lane] = of_given;
+      s_u[wave][lane] = u_all;
     }
-    s_sum[wave][lane] = sum;
-    s_given[wave][lane] = of_given;
-    s_u[wave][lane] = u_all;
-  }
-  __syncthreads();
-  if (wave == 0 && i < total) {
-    double sum = 0.0, of_given = 0.0, u_all = 0.0;
+    __syncthreads();
+    if (wave == 0 && i < total) {
+      double sum = 0.0, of_given = 0.0, u_all = 0.0;
 #pragma unroll
-    for (u32 w = 0; w < kMxEndWaves; ++w) {
-      sum += s_sum[w][lane];
-      of_given += s_given[w][lane];
-      u_all += s_u[w][lane];
+      for (u32 w = 0; w < kMxEndWaves; ++w) {
+        sum += s_sum[w][lane];
+        of_given += s_given[w][lane];
+        u_all += s_u[w][lane];
+      }
+      out[i] = (float)(scale * ((ENTROPY ? sum : -u_all * sum) + of_given));
     }
-    out[i] = (float)(scale * ((ENTROPY ? sum : -u_all * sum) + of_given));
+    __syncthreads();
   }
 }
 

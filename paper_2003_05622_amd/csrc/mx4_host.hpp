@@ -5,7 +5,7 @@ namespace {
 
 constexpr uint64_t kMxMaxQueries = 1ull << 20;
 constexpr uint64_t kMxMaxRows = (1ull << 31) - 1;
-constexpr uint64_t kMxMaxBlocks = 1ull << 30;      // workgroups a launch may have
+constexpr uint64_t kMxMaxBlocks = (1ull << 24) - 1;   // workgroups of 256 a launch may have
 constexpr uint64_t kMxMaxScores = 1ull << 40;      // scores of a call, more than a GPU has room for
 constexpr uint64_t kMxScoreGroups = 2048;          // workgroups of mx_scores that fill the GPU
 
@@ -285,6 +285,7 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
   MxGradSplit p = {};
   float* parts = static_cast<float*>(d_workspace);
   const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
+  if (rows->n == 0) d_bias = nullptr;                // (there is nothing to read behind it)
   mx_by_flag(d_bias != nullptr, [&](auto biased) {
     mx_by_flag(d_dentropy != nullptr, [&](auto with_entropy) {
       constexpr bool B = decltype(biased)::value, E = decltype(with_entropy)::value;
@@ -292,7 +293,8 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
         p = mx_grad_split(m, rows->n, dim);
         const double exact = B ? 1.4426950408889634 : std::fabs((double)scale) * 1.4426950408889634;
         const float held = B ? kMxLog2e : std::fabs(scale) * kMxLog2e;
-        const MxGradUnit unit = {held, held > 0.f ? (float)(exact / held - 1.0) : 0.f};
+        // (a unit below the normal numbers is off by much, of exponents that are next to nothing)
+        const MxGradUnit unit = {held, held > 1e-30f ? (float)(exact / held - 1.0) : 0.f};
         const dim3 grid((unsigned)p.parts, (unsigned)p.grid_queries, (unsigned)p.grid_columns);
         mx_by_shape(dim, [&](auto shape) {
           typedef decltype(shape) Shape;
@@ -317,7 +319,7 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
 #undef HPS_MX_GRADIENT
         });
       }
-      mx_gradient_end<B, E><<<(unsigned)mx_ceil(m * dim, kWave), kMxEndWaves * kWave, 0, s>>>(
+      mx_gradient_end<B, E><<<grid_for(m * dim, kWave, 1u << 20), kMxEndWaves * kWave, 0, s>>>(
           mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, d_given, d_dlogp, n_given, parts, (u32)p.sums, d_dqueries);
     });
   });

@@ -621,3 +621,70 @@ def test_an_entropy_that_is_all_there_is_to_lose():
         (q, qv), (r, rv) = make(rng, 2, 64), make(rng, 3, 64, 0.1)
         given = rng.integers(-1, 3, size=(2, 16)).astype(np.int32)
         check_gradient(q, qv, r, rv, 0.6, None, given, (0.1 * rng.normal(size=(2, 16))).astype(np.float32), rng.normal(size=2).astype(np.float32))
+
+
+@pytest.mark.parametrize("m", [3, 300])
+@pytest.mark.parametrize("n", [40, 700, 100_000])
+def test_more_equal_scores_than_there_is_room_for(m, n):
+    """All rows alike: the best are the first, whichever way they are found."""
+    rng = np.random.default_rng(n)
+    one = ref.quantize(rng.normal(size=(1, 8)).astype(np.float32))
+    r = hps.Mx4Rows(dev(np.repeat(one[0], n, axis=0)), dev(np.repeat(one[1], n, axis=0)), 8)
+    (q, _) = make(rng, m, 8)
+    for top in (1, 5, 8, 16, 17, 64):
+        got = hps.mx4_logprobs(q, r, top=top)
+        want = torch.arange(top, device="cuda", dtype=torch.int32)
+        want = torch.where(want < n, want, torch.full_like(want, -1))
+        assert (got.top_index == want).all()
+        assert (got.top_logp[:, :min(top, n)] + np.log(n)).abs().max() <= 1e-5 * np.log(n)
+
+
+@pytest.mark.parametrize("top", [1, 3, 8, 16, 33, 64])
+@pytest.mark.parametrize("n", [50, 3000, 30_000])
+def test_best_rows_of_many_queries(n, top):
+    rng = np.random.default_rng(n + top)
+    (q, qv), (r, rv) = make(rng, 300, 16), make(rng, n, 16, 0.1)
+    check_logprobs(q, qv, r, rv, 2.5, None, None, top)
+
+
+def test_backward_without_rows_reads_nothing():
+    """No rows, but a bias and given rows: called as C, since the binding has no address for an empty bias."""
+    (q, _) = make(np.random.default_rng(1), 5, 64)
+    none = hps.binding.Mx4Operand(None, None, 0)
+    bias, lse = torch.zeros(4, device="cuda"), torch.full((5,), float("-inf"), device="cuda")
+    given = torch.full((5, 2), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    given[:, 1] = -5
+    u, out = torch.ones((5, 2), device="cuda"), torch.full((5, 64), 3.0, device="cuda")
+    space = torch.empty(hps.lib().hps_mx4_logprobs_backward_bytes(5, 0, 64), dtype=torch.uint8, device="cuda")
+    st = hps.lib().hps_mx4_logprobs_backward(q._operand(), ctypes.byref(none), 64, 1.0, bias.data_ptr(), lse.data_ptr(), None, given.data_ptr(),
+                                             u.data_ptr(), 2, None, out.data_ptr(), space.data_ptr(), space.numel(),
+                                             torch.cuda.current_stream().cuda_stream)
+    assert st == hps.OK and (out == 0).all()
+
+
+def test_gradient_of_more_values_than_a_launch_has_workgroups():
+    m, n, dim = 1 << 17, 3, 1024
+    (r, rv) = make(np.random.default_rng(2), n, dim, 0.1)
+    codes = torch.randint(0, 256, (m, dim // 2), dtype=torch.uint8, device="cuda")
+    q = hps.Mx4Rows(codes, torch.full((m, dim // 32), 125, dtype=torch.uint8, device="cuda"), dim)
+    given = torch.randint(0, n, (m, 1), dtype=torch.int32, device="cuda")
+    u = torch.ones((m, 1), device="cuda")
+    out = hps.mx4_logprobs(q, r, given, scale=0.05)
+    d = hps.mx4_logprobs_backward(q, r, given, u, out.lse, out.entropy, scale=0.05)
+    for a, b in ((0, 70), (65_500, 65_600), (m - 70, m)):
+        part = q[a:b]
+        o = hps.mx4_logprobs(part, r, given[a:b], scale=0.05)
+        want = hps.mx4_logprobs_backward(part, r, given[a:b], u[a:b], o.lse, o.entropy, scale=0.05)
+        assert torch.equal(d[a:b], want)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-45, -1e-38, 1e-20, 1e6])
+def test_gradient_with_scales_of_all_sizes(scale):
+    rng = np.random.default_rng(12)
+    (q, qv), (r, rv) = make(rng, 40, 64), make(rng, 900, 64, 0.1)
+    given = rng.integers(-1, 900, size=(40, 2)).astype(np.int32)
+    if scale < 1:
+        check_gradient(q, qv, r, rv, scale, None, given, rng.normal(size=(40, 2)).astype(np.float32), rng.normal(size=40).astype(np.float32))
+    else:
+        out = hps.mx4_logprobs(q, r, dev(given), scale=scale)
+        assert torch.isfinite(out.lse).all() and (out.entropy >= -1e-6).all()
