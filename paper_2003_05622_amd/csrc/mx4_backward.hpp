@@ -15,6 +15,10 @@
 // leaves (lse is a float32 number: a p is off by 2^-24 |lse| of itself).
 // Without a gradient of the entropy c is p up to a factor per query, which the end applies.
 // mx_gradient_end adds the parts of the rows and the given rows.
+//
+// What bounds it: vector and matrix instructions, of which the GPU does hardly more than one kind at a time: 72 vector instructions (16
+// of them exponentials) and 9 of the matrix unit for 32 x 32 scores at 64 values a row, 164 us one after the other for 1024
+// queries and 0.5 M rows, 177 measured and 8 for the end.
 #pragma once
 
 #include "mx4_logprobs.hpp"
@@ -230,7 +234,9 @@ __device__ __forceinline__ void mx_store_sums(const MxTile* sum, float correct, 
 }
 
 // A workgroup: query_groups (1, 2 or 4) x QT x 32 queries, a part of the rows, of which each of 4 / query_groups groups of waves
-// takes some tiles of every stage (and has a part of its own in `parts`), and COLUMNS columns.
+// takes some tiles of every stage, and COLUMNS columns.  The groups' sums are added up in LDS, so that `parts` holds one for each
+// part of the rows: 1 query against 1 M rows, 64 wide, takes 30 us (40 with a part of its own for each group), 8 against 262 144, 16
+// wide, 16 us (27), 64 against 65 536, 64 wide, 15.5 us (20.6).
 template <typename SHAPE, bool BIAS, bool ENTROPY, int COLUMNS, int QT>
 __global__ void __launch_bounds__(kMxGradWaves * kWave) HPS_MX_WAVES
 mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, MxGradUnit unit, const float* __restrict__ bias,
@@ -311,11 +317,28 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
     unpack.store(stage0 + kMxStageRows + wave * kMxTile, end, col0, row_bytes, s_rows[buffer ^ 1u][wave]);
     __syncthreads();
   }
+  if (splits > 1) {
+    // (one query tile a wave then; the last stage's values are done with)
+    float* const of_waves = reinterpret_cast<float*>(&s_rows[0][0][0]);
+    static_assert(sizeof(s_rows) >= (kMxGradWaves - 1) * BLOCKS * 16 * kWave * sizeof(float), "");
+    if (split > 0) {
+#pragma unroll
+      for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) of_waves[(((wave - query_groups) * BLOCKS + k) * 16 + r) * kWave + lane] = sum[0][k][r];
+    }
+    __syncthreads();
+    if (split > 0) return;
+    for (u32 w = wave; w < kMxGradWaves - query_groups; w += query_groups)
+#pragma unroll
+      for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[0][k][r] += of_waves[((w * BLOCKS + k) * 16 + r) * kWave + lane];
+  }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const u32 mine = query0 + t * kMxTile;
-    if (mine < queries.n)
-      mx_store_sums<BLOCKS>(sum[t], query[t].correct, col0, dim, parts + ((u64)(blockIdx.x * splits + split) * queries.n + mine) * dim);
+    if (mine < queries.n) mx_store_sums<BLOCKS>(sum[t], query[t].correct, col0, dim, parts + ((u64)blockIdx.x * queries.n + mine) * dim);
   }
 }
 
@@ -401,13 +424,12 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
 
 // The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.  Added up in 64 bits: the two
 // may cancel almost entirely.
-constexpr u32 kMxEndWaves = 16;
-template <bool BIAS, bool ENTROPY>
-__global__ void __launch_bounds__(kMxEndWaves * kWave)
+template <bool BIAS, bool ENTROPY, u32 WAVES>
+__global__ void __launch_bounds__(WAVES * kWave)
 mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, float scale, const float* __restrict__ bias,
                 const i32* __restrict__ given, const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ parts,
                 u32 n_parts, float* __restrict__ out) {
-  __shared__ double s_sum[kMxEndWaves][kWave], s_given[kMxEndWaves][kWave], s_u[kMxEndWaves][kWave];
+  __shared__ double s_sum[WAVES][kWave], s_given[WAVES][kWave], s_u[WAVES][kWave];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave;
   const u64 total = (u64)n_queries * dim;
   for (u64 i0 = (u64)blockIdx.x * kWave; i0 < total; i0 += (u64)gridDim.x * kWave) {
@@ -416,8 +438,8 @@ mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, 
       const u32 query = (u32)(i / dim), col = (u32)(i - (u64)query * dim);
       double sum = 0.0, of_given = 0.0, u_all = 0.0;
 #pragma unroll 8
-      for (u32 p = wave; p < n_parts; p += kMxEndWaves) sum += parts[p * total + i];
-      for (u32 g = wave; g < n_given; g += kMxEndWaves) {
+      for (u32 p = wave; p < n_parts; p += WAVES) sum += parts[p * total + i];
+      for (u32 g = wave; g < n_given; g += WAVES) {
         const u64 at = (u64)query * n_given + g;
         const float u = mx_upstream<BIAS>(given, d_logp, at, rows.n, bias);
         u_all += u;
@@ -431,7 +453,7 @@ mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, 
     if (wave == 0 && i < total) {
       double sum = 0.0, of_given = 0.0, u_all = 0.0;
 #pragma unroll
-      for (u32 w = 0; w < kMxEndWaves; ++w) {
+      for (u32 w = 0; w < WAVES; ++w) {
         sum += s_sum[w][lane];
         of_given += s_given[w][lane];
         u_all += s_u[w][lane];

@@ -239,7 +239,7 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
 // The gradient's division: workgroups of up to four (narrow rows and many queries: eight) query tiles and a part of the rows each;
 // where the tiles are fewer than a workgroup's waves, these share the rows instead.
 struct MxGradSplit {
-  uint64_t wave_tiles, query_groups, grid_queries, columns, grid_columns, part_rows, parts, sums;
+  uint64_t wave_tiles, query_groups, grid_queries, columns, grid_columns, part_rows, parts;
 };
 // Whether the waves share the rows' tiles.  (Rows of more than 512 values fill the registers of a wave by themselves: 8 queries against 131 072
 // rows of 1024 take 239 us without sharing, 100 queries 211 us with it; 64 queries, 512 wide, 66 us without and 81 with it.)
@@ -256,14 +256,13 @@ static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t d
   const uint64_t wanted = std::max<uint64_t>(1, kMxGradGroups * (s.columns > 64 || s.wave_tiles == 2 ? 1 : 2) / (s.grid_queries * s.grid_columns));
   s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), kMxStageRows) * kMxStageRows;
   s.parts = mx_ceil(n_rows, s.part_rows);
-  s.sums = s.parts * (kMxGradWaves / s.query_groups);
   return s;
 }
 
 size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
   if (!mx_sizes_ok(n_queries, n_rows, dim)) return 0;
   if (n_queries == 0 || n_rows == 0) return kAlign;
-  return align_up(mx_grad_split(n_queries, n_rows, dim).sums * n_queries * dim * sizeof(float));
+  return align_up(mx_grad_split(n_queries, n_rows, dim).parts * n_queries * dim * sizeof(float));
 }
 
 hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
@@ -319,8 +318,14 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
 #undef HPS_MX_GRADIENT
         });
       }
-      mx_gradient_end<B, E><<<grid_for(m * dim, kWave, 1u << 20), kMxEndWaves * kWave, 0, s>>>(
-          mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, d_given, d_dlogp, n_given, parts, (u32)p.sums, d_dqueries);
+      const unsigned blocks_end = grid_for(m * dim, kWave, 1u << 20);
+#define HPS_MX_END(WAVES)                                                                                                    \
+  mx_gradient_end<B, E, WAVES><<<blocks_end, WAVES * kWave, 0, s>>>(mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, \
+                                                                    d_given, d_dlogp, n_given, parts, (u32)p.parts, d_dqueries)
+      // (few values: more waves each; many: as many workgroups at once as there are)
+      if (blocks_end <= 256) HPS_MX_END(16);
+      else HPS_MX_END(8);
+#undef HPS_MX_END
     });
   });
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
