@@ -75,11 +75,6 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
     mx_load_row<SHAPE>(rows, at, blocks, &r[t]);
     mx_clear_rest<SHAPE>(blocks, &r[t]);
     b[t] = BIAS ? mx_bias(bias, at) : 0.f;
-    // a row that is out has products all the same, but none that are NaN
-    if (BIAS && b[t] == -kMxInf) {
-#pragma unroll
-      for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r[t].scales[w] = 0;
-    }
   }
   const u32 left = row < rows.n ? min(rows.n - row, (u32)RT) : 0;
   const u32 tiles = (queries.n + kMxTile - 1) / kMxTile, begin = query_part * part_tiles, last = min(begin + part_tiles, tiles);
@@ -91,7 +86,7 @@ mx_scores(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __r
     auto one = [&](int i) {
       float s[RT];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) s[t] = BIAS ? __fmaf_rn(d[t][i], scale, b[t]) : __fmul_rn(d[t][i], scale);
+      for (int t = 0; t < RT; ++t) s[t] = mx_score<BIAS>(d[t][i], scale, b[t]);
       mx_store_scores<RT, BF16, WHOLE_LINES>(to + (8 * (i / 4) + i % 4) * pitch, s, left);
     };
     if (queries_left >= kMxTile) {
