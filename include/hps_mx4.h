@@ -70,7 +70,7 @@ hps_status hps_mx4_get(hps_table* t, const uint64_t* d_keys, uint64_t n, uint8_t
  * held values is summed in float32).  scale: a host value, at most 2^100 in magnitude; scores should stay
  * below 2^126 (beyond, results may be NaN).
  *   d_bias [rows] float32 or NULL.  A bias that is not finite takes its row out: its score is
- *   -infinity, whatever its codes are.  The lowest finite value is a bias like any other.
+ *   -infinity, whatever its codes and the query's are.  The lowest finite value is a bias like any other.
  * At most 2^20 queries and fewer than 2^31 rows; either may be 0. */
 
 /* All scores: d_out [queries, rows], row i `stride` values after row i - 1 (stride >= rows), float32
@@ -90,7 +90,8 @@ hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows,
  *             score - lse of the rows with the highest scores, best first, the lower number first
  *             among equal scores.  Where fewer rows are left: -1 and -infinity
  * A query that no row is left for: lse -infinity, entropy 0, logp -infinity.  A query that meets a
- * NaN score: lse, entropy, logp and top_logp are NaN, and the best rows are those among the others.
+ * NaN score: lse, entropy, logp (but -infinity of a row that is taken out, and 0 of padding) and top_logp are NaN, and
+ * the best rows are those among the others.
  *   d_workspace  hps_mx4_logprobs_bytes() bytes (0 for arguments that are not allowed), 256-byte aligned; its
  *                contents do not matter before and after.
  * Two calls with the same inputs give the same bits.  Errors: HPS_EINVAL, HPS_ENOMEM. */

@@ -353,6 +353,23 @@ __device__ __forceinline__ void mx_clear_rest(u32 blocks, MxRow<SHAPE>* row) {
     if (2 * s + half >= blocks) row->codes[s] = make_int4(0, 0, 0, 0);
 }
 
+// Whether a row of a lane's operand has a block that stands for NaN; its scales are finite ones then.  (For products whose rows may be
+// taken out: such a product is to leave no NaN, and the caller puts it where a row is left.)
+template <typename SHAPE>
+__device__ __forceinline__ bool mx_take_nan(u32 blocks, MxRow<SHAPE>* row) {
+  const u32 half = lane_id() / 32;
+  u32 nan = 0;
+#pragma unroll
+  for (int s = 0; s < SHAPE::STEPS; ++s) {
+    const u32 scale = SHAPE::PACKED ? row->scales[s / 4] >> (8 * (s % 4)) & 255u : row->scales[s];
+    nan |= 2 * s + half < blocks && scale == kMxNoScale;
+  }
+  nan |= mx_lane_xor<32>(nan);
+#pragma unroll
+  for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) row->scales[w] = nan ? 0u : row->scales[w];
+  return nan != 0;
+}
+
 // Changes the signs of all values.
 template <typename SHAPE>
 __device__ __forceinline__ void mx_negate(MxRow<SHAPE>* row) {

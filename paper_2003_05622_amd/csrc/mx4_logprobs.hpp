@@ -47,6 +47,10 @@ __device__ __forceinline__ MxPart mx_join(MxPart a, MxPart b, float unit) {
   mx_raise(&b, m, unit);
   return {m, a.l + b.l, a.e + b.e};
 }
+// The part of a query that stands for NaN, worked out with another: NaN if it has met a row that is not out.
+__device__ __forceinline__ void mx_put_nan(bool nan, MxPart* a) {
+  if (nan && a->l > 0.f) a->l = __uint_as_float(0x7FC00000u);
+}
 __device__ __forceinline__ MxPart mx_shuffle_xor(MxPart a, int distance) {
   return {__shfl_xor(a.m, distance, kWave), __shfl_xor(a.l, distance, kWave), __shfl_xor(a.e, distance, kWave)};
 }
@@ -112,6 +116,7 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
   // without a bias the maximum is taken of the products themselves: a negative scale goes into the queries' signs
   const float unit = BIAS ? kMxLog2e : fabsf(scale) * kMxLog2e;
   MxRow<SHAPE> q[QT];
+  bool nan[QT];
   MxPart sum[QT];
   float high[QT];
 #pragma unroll
@@ -119,6 +124,7 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
     mx_load_row<SHAPE>(queries, min(query0 + k * kMxTile, queries.n - 1), blocks, &q[k]);
     mx_clear_rest<SHAPE>(blocks, &q[k]);
     if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[k]);
+    nan[k] = BIAS && mx_take_nan<SHAPE>(blocks, &q[k]);
     sum[k] = mx_no_part();
     high[k] = -kMxInf;
   }
@@ -177,6 +183,7 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
 #pragma unroll
   for (int k = 0; k < QT; ++k) {
     sum[k] = mx_join(sum[k], mx_shuffle_xor(sum[k], 32), unit);
+    if (BIAS) mx_put_nan(nan[k], &sum[k]);
     const u32 query = query0 + k * kMxTile;
     if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum[k];
   }
@@ -198,6 +205,7 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
   mx_load_row<SHAPE>(queries, min(query, queries.n - 1), blocks, &q);
   mx_clear_rest<SHAPE>(blocks, &q);
   if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
+  const bool nan = BIAS && mx_take_nan<SHAPE>(blocks, &q);
   MxPart sum = mx_no_part();
   float high = -kMxInf;
   int4 own[Shared::OWN];
@@ -248,6 +256,7 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
     }
   }
   sum = mx_join(sum, mx_shuffle_xor(sum, 32), unit);
+  if (BIAS) mx_put_nan(nan, &sum);
   if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum;
 }
 

@@ -47,3 +47,25 @@ def test_scores_of_a_query_that_stands_for_nan(m, n, dim, all_out):
     assert same_or_nan(got, want)
     narrow = hps.mx4_scores(queries, rows, 0.5, bias, dtype=torch.bfloat16)
     assert same_or_nan(narrow, want.bfloat16())
+
+
+@pytest.mark.parametrize("m,n,dim", SHAPES)
+@pytest.mark.parametrize("all_out", [False, True])
+def test_log_probabilities_of_a_query_that_stands_for_nan(m, n, dim, all_out):
+    clean, queries, rows, bias, out, broken = case(m, n, dim, all_out)
+    given = torch.randint(0, n, (m, 3), dtype=torch.int32, device="cuda")
+    given[:, 0], given[:, 1] = -1, n // 2           # padding, a row that is out
+    want = hps.mx4_logprobs(clean, rows, given, 9, 0.5, bias)
+    got = hps.mx4_logprobs(queries, rows, given, 9, 0.5, bias)
+    others = torch.ones(m, dtype=torch.bool, device="cuda")
+    others[broken] = False
+    for a, b in zip(got, want):
+        assert torch.equal(a[others], b[others])
+    for i in broken:
+        assert (got.top_index[i] == -1).all() and (got.top_logp[i] == -INF).all()
+        assert got.logp[i, 0] == 0 and got.logp[i, 1] == -INF
+        if all_out:
+            assert got.lse[i] == -INF and got.entropy[i] == 0 and got.logp[i, 2] == -INF
+        else:
+            assert torch.isnan(got.lse[i]) and torch.isnan(got.entropy[i])
+            assert got.logp[i, 2] == -INF if bool(out[given[i, 2].long()]) else torch.isnan(got.logp[i, 2])
