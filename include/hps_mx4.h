@@ -109,6 +109,7 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
  *   d_given, d_dlogp  [queries, n_given] (both NULL: n_given 0); a row given twice counts twice; where d_given is no
  *                     row's number, or one of a row that is taken out, d_dlogp is not used
  *   d_dentropy        [queries] or NULL
+ * A query that no row is left for has a gradient of 0, one that meets a NaN score of NaN.
  *   d_workspace       hps_mx4_logprobs_backward_bytes() bytes, 256-byte aligned
  * Two calls with the same inputs give the same bits.  Errors: HPS_EINVAL, HPS_ENOMEM. */
 size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim);

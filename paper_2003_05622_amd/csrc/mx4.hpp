@@ -353,6 +353,13 @@ __device__ __forceinline__ void mx_clear_rest(u32 blocks, MxRow<SHAPE>* row) {
     if (2 * s + half >= blocks) row->codes[s] = make_int4(0, 0, 0, 0);
 }
 
+// A row with finite scales, whatever it stands for: its products are numbers, and are not used.
+template <typename SHAPE>
+__device__ __forceinline__ void mx_take_out(MxRow<SHAPE>* row) {
+#pragma unroll
+  for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) row->scales[w] = 0;
+}
+
 // Whether a row of a lane's operand has a block that stands for NaN; its scales are finite ones then.  (For products whose rows may be
 // taken out: such a product is to leave no NaN, and the caller puts it where a row is left.)
 template <typename SHAPE>
@@ -365,8 +372,7 @@ __device__ __forceinline__ bool mx_take_nan(u32 blocks, MxRow<SHAPE>* row) {
     nan |= 2 * s + half < blocks && scale == kMxNoScale;
   }
   nan |= mx_lane_xor<32>(nan);
-#pragma unroll
-  for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) row->scales[w] = nan ? 0u : row->scales[w];
+  if (nan) mx_take_out<SHAPE>(row);
   return nan != 0;
 }
 

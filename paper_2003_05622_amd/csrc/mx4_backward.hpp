@@ -131,11 +131,13 @@ struct MxGradUnit {
 template <bool BIAS>
 struct MxGradQuery {
   float lse, base, correct, a, b;
+  bool none;           // all rows are out
   // log2 p = x unit - base (biased: (x - lse) unit); what base leaves of lse log2 e is a factor of all p, and so, nearly, is
   // what unit leaves: x unit is lse - entropy on average.
   __device__ __forceinline__ void load(u32 query, const MxGradUnit& unit, const float* of_lse, const float* of_entropy) {
-    // (-inf: all rows are out, and any number will do)
-    lse = of_lse[query] == -kMxInf ? 0.f : of_lse[query];
+    // (any number will do where all rows are out)
+    none = of_lse[query] == -kMxInf;
+    lse = none ? 0.f : of_lse[query];
     base = lse * kMxLog2e;
     const float rest = __fmaf_rn(lse, kMxLog2e, -base) + lse * 1.92596300e-8f;
     const float x_unit = of_entropy ? base - of_entropy[query] * kMxLog2e : 0.f;
@@ -268,6 +270,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
     mx_clear_rest<SHAPE>(blocks, &q[t]);
     if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[t]);
     query[t].load(mine, unit, lse, entropy);
+    if (BIAS && query[t].none) mx_take_out<SHAPE>(&q[t]);
     if (ENTROPY) query[t].load_entropy(mine, entropy, d_entropy, given, d_logp, n_given, rows.n, bias);
 #pragma unroll
     for (int k = 0; k < BLOCKS; ++k) sum[t][k] = mx_zero_tile();
@@ -292,10 +295,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
       __builtin_amdgcn_sched_barrier(0);          // (the loads above are not to be put off until their results are wanted)
       float x_bias[16];
       if (BIAS) {
-        if (my_bias == -kMxInf) {
-#pragma unroll
-          for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) r.scales[w] = 0;
-        }
+        if (my_bias == -kMxInf) mx_take_out<SHAPE>(&r);
         __builtin_amdgcn_wave_barrier();
         s_bias[wave][lane % 32] = my_bias;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -375,6 +375,7 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
   mx_clear_rest<SHAPE>(blocks, &q);
   if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
   query.load(min(mine, queries.n - 1), unit, lse, entropy);
+  if (BIAS && query.none) mx_take_out<SHAPE>(&q);
   if (ENTROPY) query.load_entropy(min(mine, queries.n - 1), entropy, d_entropy, given, d_logp, n_given, rows.n, bias);
 #pragma unroll
   for (u32 k = 0; k < BLOCKS; ++k) sum[k] = mx_zero_tile();

@@ -1,11 +1,13 @@
 """A query with a block that stands for NaN (a pooled row that held an infinity) against rows of which some, or all, are taken out by
-their bias: a row that is out is out whatever the query holds, and the other queries notice nothing.  Compared bit for bit
-with the same call where the query is an ordinary one."""
+their bias: a row that is out is out whatever the query holds, and the other queries notice nothing.  Compared with the same call where
+the query is an ordinary one, bit for bit but for gradients: whether 32 queries' probabilities go through the matrix unit with all their
+bits, or are off by up to 2^-16 of themselves, is decided for all of them together."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2003_05622_amd as hps
+import mx4_reference as ref
 from test_gpu_mx4 import dev, make
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +71,45 @@ def test_log_probabilities_of_a_query_that_stands_for_nan(m, n, dim, all_out):
         else:
             assert torch.isnan(got.lse[i]) and torch.isnan(got.entropy[i])
             assert got.logp[i, 2] == -INF if bool(out[given[i, 2].long()]) else torch.isnan(got.logp[i, 2])
+
+
+@pytest.mark.parametrize("m,n,dim", SHAPES)
+@pytest.mark.parametrize("all_out", [False, True])
+@pytest.mark.parametrize("with_entropy", [False, True])
+def test_gradient_of_a_query_that_stands_for_nan(m, n, dim, all_out, with_entropy):
+    clean, queries, rows, bias, out, broken = case(m, n, dim, all_out)
+    given = torch.randint(0, n, (m, 2), dtype=torch.int32, device="cuda")
+    u = torch.randn((m, 2), device="cuda")
+    h = torch.randn(m, device="cuda") if with_entropy else None
+    fine = hps.mx4_logprobs(clean, rows, given, 0, 0.5, bias)
+    want = hps.mx4_logprobs_backward(clean, rows, given, u, fine.lse, fine.entropy, h, 0.5, bias)
+    # (lse and entropy as documented for such a query, whatever the forward pass gives)
+    lse, entropy = fine.lse.clone(), fine.entropy.clone()
+    lse[broken], entropy[broken] = (-INF, 0.0) if all_out else (float("nan"), float("nan"))
+    got = hps.mx4_logprobs_backward(queries, rows, given, u, lse, entropy, h, 0.5, bias)
+    others = torch.ones(m, dtype=torch.bool, device="cuda")
+    others[broken] = False
+    # |c_r| <= p_r (|U| + |h| (|log p_r| + H)), of which 2^-16 may be missing on either side
+    s = hps.mx4_scores(clean, rows, 0.5, bias)
+    deep = torch.where(s == -INF, 0.0, (s - fine.lse[:, None]).abs()).nan_to_num(nan=0.0).amax(1) + fine.entropy
+    size = u.abs().sum(1) + (h.abs() * deep if with_entropy else 0.0)
+    off = 2 * 2.0 ** -16 * 0.5 * size * rows.dequantize().abs().max()
+    assert ((got - want).abs() <= off[:, None])[others].all()
+    for i in broken:
+        assert (got[i] == 0).all() if all_out else torch.isnan(got[i]).all()
+
+
+def test_a_pooled_row_that_is_not_finite_goes_through():
+    """From values: an infinity makes its block NaN, and rows that are out stay out behind it."""
+    rng = np.random.default_rng(3)
+    x = torch.randn((4, 64), device="cuda")
+    x[2, 40] = INF
+    rows, _ = make(rng, 50, 64, 0.1)
+    bias = torch.full((50,), -INF, device="cuda")
+    queries = hps.mx4_quantize(x)
+    assert queries.scales.cpu().tolist()[2][1] == 255
+    got = hps.mx4_logprobs(queries, rows, None, 3, 1.0, bias)
+    assert (got.lse == -INF).all() and (got.entropy == 0).all() and (got.top_index == -1).all()
+    d = hps.mx4_logprobs_backward(queries, rows, None, None, got.lse, got.entropy, torch.ones(4, device="cuda"), 1.0, bias)
+    assert (d == 0).all() and (hps.mx4_scores(queries, rows, 1.0, bias) == -INF).all()
+    assert np.isneginf(ref.scores(np.full((1, 64), np.nan), np.zeros((50, 64)), 1.0, bias.cpu().numpy())).all()
