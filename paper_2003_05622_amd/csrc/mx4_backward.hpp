@@ -8,11 +8,14 @@
 // query, c of which is at once the second operand of the product with the rows' values (which rows a step of the
 // matrix instruction takes, in which order, is free as long as both operands agree).  The values, exact in
 // bfloat16, are unpacked into LDS by the workgroup, in the order the first operand wants them: lane l of a step holds
-// column l % 32 of eight rows.  c goes through the matrix instruction in bfloat16 pieces: the sum over the rows, together
-// with the given ones, is what little is left of large terms, and eight bits would show.  Three pieces add up to c's 24 bits
-// exactly, two are off by 2^-18 of it at most.  Where p is above 2^-6 all three are used, which a query has at most 64 rows for;
-// the others' errors, independent of each other, come to 2^-18 sqrt(sum p^2) <= 2^-21 of a row at most, as float32 itself
-// leaves (lse is a float32 number: a p is off by 2^-24 |lse| of itself).
+// column l % 32 of eight rows.  c goes through the matrix instruction in bfloat16 pieces, each the nearest to what the ones before it
+// leave: the sum over the rows, together with the given ones, is what little is left of large terms, and eight bits would show.
+// Three pieces add up to c's 24 bits exactly; two leave 2^-17 of it at most, 2^-18.7 in the mean square over all fractions.  All
+// three are used where p is above 2^-6, which a query has at most 64 rows for.  The others' errors, independent of each other as long
+// as the probabilities differ, come to 2^-18.7 sqrt(sum p^2) <= 2^-21.7 of a row, as float32 itself leaves (lse is a float32 number:
+// a p is off by 2^-24 |lse| of itself).  Equal probabilities have equal errors, which add up (a query of zeros has nothing else):
+// all three are used too where rows of a tile have the same p.  That test takes 1.5 % of the time.  What no test sees (probabilities of a few sizes that
+// take turns) stays below 2^-17 sum p |row|.
 // Without a gradient of the entropy c is p up to a factor per query, which the end applies.
 // mx_gradient_end adds the parts of the rows and the given rows.
 //
@@ -169,16 +172,18 @@ template <bool BIAS, bool ENTROPY, int BLOCKS>
 __device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float scale, const MxGradQuery<BIAS>& query, float unit,
                                             const uint2* values, const MxOnes& ones, MxTile* sum) {
   const u32 lane = lane_id();
-  float most = 0.f;
+  float p[16], most = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float log2_p = BIAS ? (__fmaf_rn(d[i], scale, x_bias[i]) - query.lse) * unit : __fmaf_rn(d[i], unit, -query.base);
-    const float p = exp2_fast(log2_p);
-    most = fmaxf(most, p);
+    p[i] = exp2_fast(log2_p);
+    most = fmaxf(most, p[i]);
     // (log p of a row far below, or out, is not multiplied with: its p is 0)
-    d[i] = ENTROPY ? p * __fmaf_rn(query.b, BIAS ? fmaxf(log2_p, -200.f) : log2_p, query.a) : p;
+    d[i] = ENTROPY ? p[i] * __fmaf_rn(query.b, BIAS ? fmaxf(log2_p, -200.f) : log2_p, query.a) : p[i];
   }
-  const bool all_pieces = __any(most > kMxLarge);
+  // (two pairs: one alone is equal by chance in some tiles of a hundred)
+  const bool alike = p[0] == p[4] && p[1] == p[5] && p[0] > 0.f;
+  const bool all_pieces = __any(most > kMxLarge || alike);
 #pragma unroll
   for (int step = 0; step < 2; ++step) {
     MxHalves8 value[BLOCKS];
@@ -190,10 +195,14 @@ __device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float
       for (int k = 0; k < BLOCKS; ++k)
         sum[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[k], __builtin_bit_cast(MxHalves8, w), sum[k], 0, 0, 0);
     };
-    // pairs of rows: the upper halves of both; what they leave (c - 1 x piece in one instruction, exactly), rounded;
+    // pairs of rows: both rounded to the nearest; what that leaves (c - 1 x piece in one instruction, exactly), likewise;
     // and what that leaves
     float c[8];
     u32 piece[4];
+    auto nearest = [&] {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+    };
     auto take_off = [&] {
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
@@ -204,17 +213,14 @@ __device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float
     };
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = d[8 * step + i];
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) piece[i / 2] = __builtin_amdgcn_perm(__float_as_uint(c[i + 1]), __float_as_uint(c[i]), 0x07060302u);
+    nearest();
     add(piece);
     take_off();
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+    nearest();
     add(piece);
     if (all_pieces) {
       take_off();
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) piece[i / 2] = mx_halves(c[i], c[i + 1]);
+      nearest();
       add(piece);
     }
   }
