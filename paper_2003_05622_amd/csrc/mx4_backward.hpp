@@ -31,6 +31,9 @@ namespace hps {
 constexpr u32 kMxStageTiles = 4;                         // tiles of 32 rows unpacked at a time
 constexpr u32 kMxStageRows = kMxStageTiles * kMxTile;
 constexpr u32 kMxGradWaves = 4;
+// Rows whose sums a wave holds in 32 bits: the matrix instruction cuts off what does not fit, always towards 0, so that 1 M equal terms
+// lose 3e-3 of their sum one after the other, and 4096 of them 1e-5.  Longer parts go on in the workspace, in 64 bits.
+constexpr u32 kMxSumRows = 4096;
 constexpr float kMxLarge = 0x1p-6f;
 
 typedef __bf16 MxHalves2 __attribute__((ext_vector_type(2)));
@@ -226,18 +229,42 @@ __device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float
   }
 }
 
-// Writes a query's sums of COLUMNS columns.
+// A launch takes up to kMxSumRows rows of each part, from number `done` of the part on.  Where the parts have more (`wide`), a
+// workgroup adds its sums to the 64-bit ones that the launches before have left.
+struct MxPartRows {
+  u32 rows, done;
+  bool wide;
+  __device__ __forceinline__ u32 first() const { return blockIdx.x * rows + done; }
+  __device__ __forceinline__ u32 end(u32 n) const {
+    const u32 start = blockIdx.x * rows, all = min(n - start, rows);
+    return start + (wide ? min(done + kMxSumRows, all) : all);
+  }
+};
+
+// Writes a query's sums of COLUMNS columns, at number `at` and following.
 template <int BLOCKS>
-__device__ __forceinline__ void mx_store_sums(const MxTile* sum, float correct, u32 col0, u32 dim, float* to) {
+__device__ __forceinline__ void mx_store_sums(const MxTile* sum, float correct, u32 col0, u32 dim, const MxPartRows& part, void* parts, u64 at) {
   const u32 half = lane_id() / 32;
 #pragma unroll
   for (int k = 0; k < BLOCKS; ++k)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const u32 col = col0 + k * 32 + 8 * g + 4 * half;
-      if (col < dim)
-        *reinterpret_cast<float4*>(to + col) =
-            make_float4(sum[k][4 * g] * correct, sum[k][4 * g + 1] * correct, sum[k][4 * g + 2] * correct, sum[k][4 * g + 3] * correct);
+      if (col >= dim) continue;
+      const float4 v = make_float4(sum[k][4 * g] * correct, sum[k][4 * g + 1] * correct, sum[k][4 * g + 2] * correct, sum[k][4 * g + 3] * correct);
+      if (!part.wide) {
+        *reinterpret_cast<float4*>(static_cast<float*>(parts) + at + col) = v;
+        continue;
+      }
+      double2* const to = reinterpret_cast<double2*>(static_cast<double*>(parts) + at + col);
+      double2 low = make_double2(v.x, v.y), high = make_double2(v.z, v.w);
+      if (part.done) {
+        const double2 l = to[0], h = to[1];
+        low = make_double2(l.x + low.x, l.y + low.y);
+        high = make_double2(h.x + high.x, h.y + high.y);
+      }
+      to[0] = low;
+      to[1] = high;
     }
 }
 
@@ -249,7 +276,7 @@ template <typename SHAPE, bool BIAS, bool ENTROPY, int COLUMNS, int QT>
 __global__ void __launch_bounds__(kMxGradWaves * kWave) HPS_MX_WAVES
 mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, MxGradUnit unit, const float* __restrict__ bias,
             const float* __restrict__ lse, const float* __restrict__ entropy, const i32* __restrict__ given, const float* __restrict__ d_logp,
-            u32 n_given, const float* __restrict__ d_entropy, u32 query_groups, u32 part_rows, float* __restrict__ parts) {
+            u32 n_given, const float* __restrict__ d_entropy, u32 query_groups, MxPartRows part, void* __restrict__ parts) {
   constexpr int BLOCKS = COLUMNS / 32;
   constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;           // of 8 bytes, a tile's unpacked values
   __shared__ uint2 s_rows[2][kMxStageTiles][kTileWords];
@@ -257,7 +284,8 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
   const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const u32 splits = kMxGradWaves / query_groups, split = wave / query_groups;
   const u32 query0 = (blockIdx.y * query_groups + wave % query_groups) * (QT * kMxTile) + lane % 32;
-  const u32 first = blockIdx.x * part_rows, end = min(rows.n - first, part_rows) + first, col0 = blockIdx.z * COLUMNS;
+  const u32 first = part.first(), end = part.end(rows.n), col0 = blockIdx.z * COLUMNS;
+  if (first >= end) return;             // (the last part is shorter)
 
   MxUnpack<COLUMNS, BIAS> unpack;
   unpack.load(rows, first + wave * kMxTile, col0, row_bytes, blocks, bias);
@@ -344,7 +372,7 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const u32 mine = query0 + t * kMxTile;
-    if (mine < queries.n) mx_store_sums<BLOCKS>(sum[t], query[t].correct, col0, dim, parts + ((u64)blockIdx.x * queries.n + mine) * dim);
+    if (mine < queries.n) mx_store_sums<BLOCKS>(sum[t], query[t].correct, col0, dim, part, parts, ((u64)blockIdx.x * queries.n + mine) * dim);
   }
 }
 
@@ -354,7 +382,7 @@ template <typename SHAPE, bool BIAS, bool ENTROPY>
 __global__ void __launch_bounds__(kMxThreads) HPS_MX_WAVES
 mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, float scale, MxGradUnit unit, const float* __restrict__ bias,
                    const float* __restrict__ lse, const float* __restrict__ entropy, const i32* __restrict__ given,
-                   const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ d_entropy, u32 part_rows, float* __restrict__ parts) {
+                   const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ d_entropy, MxPartRows part, void* __restrict__ parts) {
   constexpr u32 COLUMNS = 128, BLOCKS = COLUMNS / 32, kStage = 2;
   constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;
   typedef MxShared<SHAPE> Shared;
@@ -363,7 +391,8 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
   __shared__ float s_bias[2][kMxTile];
   const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const u32 mine = (blockIdx.y * (kMxThreads / kWave) + wave) * kMxTile + lane % 32;
-  const u32 first = blockIdx.x * part_rows, end = min(rows.n - first, part_rows) + first, col0 = blockIdx.z * COLUMNS;
+  const u32 first = part.first(), end = part.end(rows.n), col0 = blockIdx.z * COLUMNS;
+  if (first >= end) return;             // (the last part is shorter)
   const u32 my_tile = wave / 2 * kMxTile, my_col = col0 + wave % 2 * (COLUMNS / 2), my_words = wave % 2 * (kTileWords / 2);
 
   MxUnpack<COLUMNS / 2, BIAS> unpack;
@@ -426,7 +455,7 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
     }
     unpack.store(stage0 + kStage * kMxTile + my_tile, end, my_col, row_bytes, s_rows[buffer ^ 1u][wave / 2] + my_words);
   }
-  if (mine < queries.n) mx_store_sums<(int)BLOCKS>(sum, query.correct, col0, dim, parts + ((u64)blockIdx.x * queries.n + mine) * dim);
+  if (mine < queries.n) mx_store_sums<(int)BLOCKS>(sum, query.correct, col0, dim, part, parts, ((u64)blockIdx.x * queries.n + mine) * dim);
 }
 
 // The end: a workgroup takes 64 of the output's values; its waves share the parts and the given rows.  Added up in 64 bits: the two
@@ -434,8 +463,8 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
 template <bool BIAS, bool ENTROPY, u32 WAVES>
 __global__ void __launch_bounds__(WAVES * kWave)
 mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, float scale, const float* __restrict__ bias,
-                const i32* __restrict__ given, const float* __restrict__ d_logp, u32 n_given, const float* __restrict__ parts,
-                u32 n_parts, float* __restrict__ out) {
+                const i32* __restrict__ given, const float* __restrict__ d_logp, u32 n_given, const void* __restrict__ parts,
+                u32 n_parts, bool wide, float* __restrict__ out) {
   __shared__ double s_sum[WAVES][kWave], s_given[WAVES][kWave], s_u[WAVES][kWave];
   const u32 lane = lane_id(), wave = threadIdx.x / kWave;
   const u64 total = (u64)n_queries * dim;
@@ -444,8 +473,12 @@ mx_gradient_end(MxHeld rows, u32 n_queries, u32 dim, u32 blocks, u32 row_bytes, 
     if (i < total) {
       const u32 query = (u32)(i / dim), col = (u32)(i - (u64)query * dim);
       double sum = 0.0, of_given = 0.0, u_all = 0.0;
+      if (wide) {
+        for (u32 p = wave; p < n_parts; p += WAVES) sum += static_cast<const double*>(parts)[p * total + i];
+      } else {
 #pragma unroll 8
-      for (u32 p = wave; p < n_parts; p += WAVES) sum += parts[p * total + i];
+        for (u32 p = wave; p < n_parts; p += WAVES) sum += static_cast<const float*>(parts)[p * total + i];
+      }
       for (u32 g = wave; g < n_given; g += WAVES) {
         const u64 at = (u64)query * n_given + g;
         const float u = mx_upstream<BIAS>(given, d_logp, at, rows.n, bias);

@@ -240,6 +240,7 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
 // where the tiles are fewer than a workgroup's waves, these share the rows instead.
 struct MxGradSplit {
   uint64_t wave_tiles, query_groups, grid_queries, columns, grid_columns, part_rows, parts;
+  bool wide;                 // parts so long that their sums are held in 64 bits
 };
 // Whether the waves share the rows' tiles.  (Rows of more than 512 values fill the registers of a wave by themselves: 8 queries against 131 072
 // rows of 1024 take 239 us without sharing, 100 queries 211 us with it; 64 queries, 512 wide, 66 us without and 81 with it.)
@@ -255,14 +256,18 @@ static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t d
   s.grid_columns = mx_ceil(dim, s.columns);
   const uint64_t wanted = std::max<uint64_t>(1, kMxGradGroups * (s.columns > 64 || s.wave_tiles == 2 ? 1 : 2) / (s.grid_queries * s.grid_columns));
   s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), kMxStageRows) * kMxStageRows;
+  // (waves that share the rows join their sums at the end of the part: each has so many rows at most)
+  if (s.query_groups < kMxGradWaves) s.part_rows = std::min<uint64_t>(s.part_rows, kMxSumRows * (kMxGradWaves / s.query_groups));
   s.parts = mx_ceil(n_rows, s.part_rows);
+  s.wide = s.query_groups == kMxGradWaves && s.part_rows > kMxSumRows;
   return s;
 }
 
 size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
   if (!mx_sizes_ok(n_queries, n_rows, dim)) return 0;
   if (n_queries == 0 || n_rows == 0) return kAlign;
-  return align_up(mx_grad_split(n_queries, n_rows, dim).parts * n_queries * dim * sizeof(float));
+  const MxGradSplit p = mx_grad_split(n_queries, n_rows, dim);
+  return align_up(p.parts * n_queries * dim * (p.wide ? sizeof(double) : sizeof(float)));
 }
 
 hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
@@ -282,7 +287,6 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
   if (workspace_bytes < hps_mx4_logprobs_backward_bytes(m, rows->n, dim)) return HPS_ENOMEM;
   hipStream_t s = static_cast<hipStream_t>(stream);
   MxGradSplit p = {};
-  float* parts = static_cast<float*>(d_workspace);
   const u32 blocks = mx_blocks(dim), row_bytes = mx_row_bytes(dim);
   if (rows->n == 0) d_bias = nullptr;                // (there is nothing to read behind it)
   mx_by_flag(d_bias != nullptr, [&](auto biased) {
@@ -295,17 +299,18 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
         // (a unit below the normal numbers is off by much, of exponents that are next to nothing)
         const MxGradUnit unit = {held, held > 1e-30f ? (float)(exact / held - 1.0) : 0.f};
         const dim3 grid((unsigned)p.parts, (unsigned)p.grid_queries, (unsigned)p.grid_columns);
-        mx_by_shape(dim, [&](auto shape) {
+        MxPartRows part = {(u32)p.part_rows, 0, p.wide};
+        auto launch = [&](auto shape) {
           typedef decltype(shape) Shape;
 #define HPS_MX_GRADIENT(COLUMNS, QT)                                                                                         \
   mx_gradient<Shape, B, E, COLUMNS, QT><<<grid, kMxGradWaves * kWave, 0, s>>>(                                               \
       mx_held(queries), mx_held(rows), dim, blocks, row_bytes, scale, unit, d_bias, d_lse, d_entropy, d_given, d_dlogp,      \
-      n_given, d_dentropy, (u32)p.query_groups, (u32)p.part_rows, parts)
+      n_given, d_dentropy, (u32)p.query_groups, part, d_workspace)
           if constexpr (Shape::STEPS >= 8) {
             if (mx_gradient_shares(m, dim)) {
               mx_gradient_shared<Shape, B, E><<<grid, kMxThreads, 0, s>>>(
                   mx_held(queries), mx_held(rows), dim, blocks, row_bytes, scale, unit, d_bias, d_lse, d_entropy, d_given, d_dlogp,
-                  n_given, d_dentropy, (u32)p.part_rows, parts);
+                  n_given, d_dentropy, part, d_workspace);
               return;
             }
           }
@@ -316,12 +321,17 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
             else if constexpr (Shape::WIDTH == 16) { if (p.wave_tiles == 2) HPS_MX_GRADIENT(64, 2); else HPS_MX_GRADIENT(64, 1); }
           }
 #undef HPS_MX_GRADIENT
-        });
+        };
+        // (part_rows is at most 2^31)
+        do {
+          mx_by_shape(dim, launch);
+          part.done += kMxSumRows;
+        } while (p.wide && part.done < p.part_rows);
       }
       const unsigned blocks_end = grid_for(m * dim, kWave, 1u << 20);
 #define HPS_MX_END(WAVES)                                                                                                    \
   mx_gradient_end<B, E, WAVES><<<blocks_end, WAVES * kWave, 0, s>>>(mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, \
-                                                                    d_given, d_dlogp, n_given, parts, (u32)p.parts, d_dqueries)
+                                                                    d_given, d_dlogp, n_given, d_workspace, (u32)p.parts, p.wide, d_dqueries)
       // (few values: more waves each; many: as many workgroups at once as there are)
       if (blocks_end <= 256) HPS_MX_END(16);
       else HPS_MX_END(8);

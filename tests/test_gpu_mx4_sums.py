@@ -4,7 +4,7 @@ Tolerances, in H = 2^-24, relative to sum p |row|.  The reference takes the same
 p: an exponential (2 H), a factor for what float32 does not hold of the exponent's parts, its exponential and its product (2 + 1 H).
 The exponent itself is off by its rounding, H |s - lse| (with a bias twice, and its unit by H / 2 of it).  Three pieces of p are exact.  An instruction
 adds 16 rows of one piece and is off by 2 H of the sum at most, one after the other in a part of the rows: 6 H / 16 a row.  Up to three
-sums of waves are joined (3 H); parts are added in 64 bits.  Together T = 8 H + 3 H |s - lse| + 6 H ceil(rows / 16).
+sums of waves are joined (3 H); parts are added in 64 bits, and so is what a long part has for every 4096 rows.  Together T = 8 H + 3 H |s - lse| + 6 H ceil(rows / 16).
 """
 import math
 
@@ -34,7 +34,7 @@ def zeros(m, dim):
 def rows_of_a_part(m, n, dim):
     """At most so many rows are added up one after the other in 32 bits: those of a part, of which the workspace has one sum for every query's value."""
     parts = hps.lib().hps_mx4_logprobs_backward_bytes(m, n, dim) // (4 * m * dim)
-    return min(n, -(-(-(-n // parts)) // 128) * 128)
+    return min(n, 4096, -(-(-(-n // parts)) // 128) * 128)
 
 
 @pytest.mark.parametrize("m,dim", [(1, 16), (1, 64), (40, 128), (70, 300), (300, 64), (3, 1024)])
@@ -85,3 +85,58 @@ def test_two_probabilities_add_up():
         want = v * (1 - p.sum())
         t = H * (8 + 3 * (float(lse) + 0.3) + 6 * math.ceil(rows_of_a_part(2, n, 64) / 16))
         assert np.all(np.abs(d - want) <= t * np.abs(v) + 2 * H * np.abs(want)), (n, np.abs(d - want).max() / H)
+
+
+# (queries, rows, dim): so many queries that one part holds all of the rows, or nearly; waves that hold two query tiles and one, and waves that share the rows
+LONG = [(131072, 300007, 16), (131077, 70001, 64), (65540, 40001, 128), (32768, 20011, 300), (8200, 8193, 1024), (8200, 12288, 1000)]
+
+
+@pytest.mark.parametrize("m,n,dim", LONG)
+@pytest.mark.parametrize("biased", [False, True])
+def test_very_many_rows_in_one_part(m, n, dim, biased):
+    # (8 bytes of workspace for each value of a query: one part, in 64 bits)
+    assert hps.lib().hps_mx4_logprobs_backward_bytes(m, n, dim) <= 8 * m * dim + 256
+    given, u = torch.zeros((m, 1), dtype=torch.int32, device="cuda"), torch.ones((m, 1), device="cuda")
+    rows, v = alike(n, dim)
+    lse = np.float32(math.log(n))
+    q = zeros(1, dim)
+    q = hps.Mx4Rows(q.codes.repeat(m, 1), q.scales.repeat(m, 1), dim)
+    d = hps.mx4_logprobs_backward(q, rows, given, u, torch.full((m,), float(lse), device="cuda"),
+                                  bias=torch.zeros(n, device="cuda") if biased else None)
+    assert torch.equal(d, d[:1].expand(m, dim))
+    d = d[0].cpu().numpy()
+    want = v * (1 - n * math.exp(-float(lse)))
+    t = H * (8 + 3 * math.log(n) + 6 * 4096 / 16)
+    assert np.all(np.abs(d - want) <= t * np.abs(v) + 2 * H * np.abs(want)), np.abs(d - want).max() / H
+
+
+@pytest.mark.parametrize("m,n,dim", [(65600, 20011, 64), (8300, 8300, 260), (65536, 4097, 16)])
+@pytest.mark.parametrize("kind", ["plain", "entropy", "biased"])
+def test_long_parts_give_what_short_ones_give(m, n, dim, kind):
+    """Some of many queries against the same ones alone, whose parts are short."""
+    rng = np.random.default_rng(n)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    q = hps.mx4_quantize(torch.randn((m, dim), generator=gen, device="cuda"))
+    r = hps.mx4_quantize(0.1 * torch.randn((n, dim), generator=gen, device="cuda"))
+    scale = 20 / math.sqrt(dim)
+    bias = None
+    if kind == "biased":
+        bias = torch.randn(n, generator=gen, device="cuda")
+        bias[dev(rng.random(n) < 0.2)] = float("-inf")
+    given = torch.randint(-1, n, (m, 2), generator=gen, device="cuda", dtype=torch.int32)
+    u = torch.randn((m, 2), generator=gen, device="cuda")
+    h = None if kind == "plain" else torch.randn(m, generator=gen, device="cuda")
+    parts = [(0, 40), (m // 2 - 5, m // 2 + 30), (m - 33, m)]
+    outs = [hps.mx4_logprobs(q[a:b], r, given[a:b], 0, scale, bias) for a, b in parts]
+    lse, entropy = torch.zeros(m, device="cuda"), torch.zeros(m, device="cuda")
+    for (a, b), out in zip(parts, outs):
+        lse[a:b], entropy[a:b] = out.lse, out.entropy
+    d = hps.mx4_logprobs_backward(q, r, given, u, lse, entropy, h, scale, bias)
+    most = r.dequantize().abs().max().item()
+    for (a, b), out in zip(parts, outs):
+        want = hps.mx4_logprobs_backward(q[a:b], r, given[a:b], u[a:b], out.lse, out.entropy, None if h is None else h[a:b], scale, bias)
+        # |c| sums up to |U| + |h| sum p |log p + H| <= |U| + 2 |h| H; sums of 4096 rows are off by 6 H / 16 a row, of pieces 2^-17 may be left out
+        size = u[a:b].abs().sum(1) + (2 * h[a:b].abs() * out.entropy if h is not None else 0.0)
+        off = abs(scale) * most * size * (2 * 6 * H * 4096 / 16 + 2 * 2.0 ** -17)
+        assert ((d[a:b] - want).abs() <= off[:, None]).all()
