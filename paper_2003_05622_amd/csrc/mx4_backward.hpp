@@ -154,12 +154,12 @@ struct MxGradQuery {
   // With a gradient of the entropy: c = p (a + b log2 p).
   __device__ __forceinline__ void load_entropy(u32 query, const float* entropy, const float* d_entropy, const i32* given, const float* d_logp,
                                                u32 n_given, u32 n_rows, const float* bias) {
-    float u = 0.f;
+    double u = 0.0;
 #pragma unroll 8
     for (u32 g = lane_id() / 32; g < n_given; g += 2) u += mx_upstream<BIAS>(given, d_logp, (u64)query * n_given + g, n_rows, bias);
     u += __shfl_xor(u, 32, kWave);
     const float h = d_entropy[query];
-    a = -__fmaf_rn(h, entropy[query], u);
+    a = (float)-((double)h * entropy[query] + u);
     b = -h * kMxLn2;
   }
 };

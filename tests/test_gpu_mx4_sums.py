@@ -140,3 +140,25 @@ def test_long_parts_give_what_short_ones_give(m, n, dim, kind):
         size = u[a:b].abs().sum(1) + (2 * h[a:b].abs() * out.entropy if h is not None else 0.0)
         off = abs(scale) * most * size * (2 * 6 * H * 4096 / 16 + 2 * 2.0 ** -17)
         assert ((d[a:b] - want).abs() <= off[:, None]).all()
+
+
+def test_very_many_given_rows():
+    """Their gradients are added up in 64 bits, with a gradient of the entropy as without."""
+    m, n, dim, g = 3, 40, 64, 300001
+    rng = np.random.default_rng(5)
+    (q, qv), (r, rv) = make(rng, m, dim, 0.3, 0.0), make(rng, n, dim, 0.3, 0.0)
+    out = hps.mx4_logprobs(q, r, scale=0.1)
+    given = rng.integers(0, n, size=(m, g)).astype(np.int32)
+    u = np.full((m, g), 0.1, dtype=np.float32)
+    s = ref.scores(qv, rv, 0.1)
+    p = np.exp(s - out.lse.cpu().numpy().astype(np.float64)[:, None])
+    total = g * float(np.float32(0.1))
+    c = -total * p
+    for i in range(m):
+        np.add.at(c[i], given[i], float(np.float32(0.1)))
+    want = float(np.float32(0.1)) * (c @ rv)
+    t = H * (8 + 3 * (np.abs(s).max() + math.log(n)) + 6 * math.ceil(n / 16) + 2)
+    off = 0.1 * total * t * (p @ np.abs(rv)) + 2 * H * np.abs(want)
+    for h in (None, torch.zeros(m, device="cuda")):
+        d = hps.mx4_logprobs_backward(q, r, dev(given), dev(u), out.lse, out.entropy, h, scale=0.1).cpu().numpy()
+        assert np.all(np.abs(d - want) <= off), np.max(np.abs(d - want) / off)
