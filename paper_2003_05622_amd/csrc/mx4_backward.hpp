@@ -31,9 +31,8 @@ namespace hps {
 constexpr u32 kMxStageTiles = 4;                         // tiles of 32 rows unpacked at a time
 constexpr u32 kMxStageRows = kMxStageTiles * kMxTile;
 constexpr u32 kMxGradWaves = 4;
-// Rows whose sums a wave holds in 32 bits: the matrix instruction cuts off what does not fit, always towards 0, so that 1 M equal terms
-// lose 3e-3 of their sum one after the other, and 4096 of them 1e-5.  Longer parts go on in the workspace, in 64 bits.
-constexpr u32 kMxSumRows = 4096;
+// (Of kMxSumRows equal terms the matrix instruction, which cuts off what does not fit, always towards 0, loses 1e-5; of 1 M, added up one
+// after the other, 3e-3.  The sums of longer parts go on in the workspace, in 64 bits.)
 constexpr float kMxLarge = 0x1p-6f;
 
 typedef __bf16 MxHalves2 __attribute__((ext_vector_type(2)));

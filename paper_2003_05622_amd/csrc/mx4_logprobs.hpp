@@ -51,6 +51,24 @@ __device__ __forceinline__ MxPart mx_join(MxPart a, MxPart b, float unit) {
 __device__ __forceinline__ void mx_put_nan(bool nan, MxPart* a) {
   if (nan && a->l > 0.f) a->l = __uint_as_float(0x7FC00000u);
 }
+
+// Rows of a part whose sums a wave holds in 32 bits.  (With many queries a part has millions: added up one after the other, their sum is off by 3e-4 at
+// 2 M rows, 2e-6 like this.)
+constexpr u32 kMxSumRows = 4096;
+
+// The sums of the rows before those, in 64 bits.
+struct MxLongPart {
+  double l, e;
+  float m;
+};
+__device__ __forceinline__ MxLongPart mx_no_long_part() { return {0.0, 0.0, kMxLowest}; }
+// Adds a lane's sums (m of which is the highest so far) and begins new ones.
+__device__ __forceinline__ void mx_put_by(MxPart* a, float unit, MxLongPart* to) {
+  const float by = (to->m - a->m) * unit;
+  const double f = exp2f(by), e = f == 0.0 ? 0.0 : (to->e + to->l * by) * f;
+  *to = {to->l * f + a->l, e + a->e, a->m};
+  a->l = a->e = 0.f;
+}
 __device__ __forceinline__ MxPart mx_shuffle_xor(MxPart a, int distance) {
   return {__shfl_xor(a.m, distance, kWave), __shfl_xor(a.l, distance, kWave), __shfl_xor(a.e, distance, kWave)};
 }
@@ -110,6 +128,7 @@ __global__ void __launch_bounds__(kWave) HPS_MX_WAVES
 mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, u32 part_rows, u32 group,
            u32 n_groups, MxPart* __restrict__ parts, float* __restrict__ highest) {
   __shared__ float s_bias[kMxTile];
+  __shared__ MxLongPart s_long[QT][kWave];
   const u32 lane = lane_id(), half = lane / 32, part = blockIdx.x;
   const u32 query0 = blockIdx.y * (QT * kMxTile) + lane % 32;
   const u32 first = part * part_rows, end = min(rows.n - first, part_rows) + first;
@@ -126,6 +145,7 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
     if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q[k]);
     nan[k] = BIAS && mx_take_nan<SHAPE>(blocks, &q[k]);
     sum[k] = mx_no_part();
+    s_long[k][lane] = mx_no_long_part();
     high[k] = -kMxInf;
   }
   MxRow<SHAPE> next;
@@ -179,9 +199,15 @@ mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __
         high[k] = -kMxInf;
       }
     }
+    if ((row0 - first) % kMxSumRows == kMxSumRows - kMxTile) {
+#pragma unroll
+      for (int k = 0; k < QT; ++k) mx_put_by(&sum[k], unit, &s_long[k][lane]);
+    }
   }
 #pragma unroll
   for (int k = 0; k < QT; ++k) {
+    mx_put_by(&sum[k], unit, &s_long[k][lane]);
+    sum[k] = {sum[k].m, (float)s_long[k][lane].l, (float)s_long[k][lane].e};
     sum[k] = mx_join(sum[k], mx_shuffle_xor(sum[k], 32), unit);
     if (BIAS) mx_put_nan(nan[k], &sum[k]);
     const u32 query = query0 + k * kMxTile;
@@ -197,6 +223,7 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
   typedef MxShared<SHAPE> Shared;
   __shared__ int4 s_tile[2][Shared::UNITS];
   __shared__ float s_bias[2][kMxTile];
+  __shared__ MxLongPart s_long[kMxThreads];
   const u32 lane = lane_id(), half = lane / 32, part = blockIdx.x;
   const u32 query = (blockIdx.y * (kMxThreads / kWave) + threadIdx.x / kWave) * kMxTile + lane % 32;
   const u32 first = part * part_rows, end = min(rows.n - first, part_rows) + first;
@@ -207,6 +234,7 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
   if (!BIAS && scale < 0.f) mx_negate<SHAPE>(&q);
   const bool nan = BIAS && mx_take_nan<SHAPE>(blocks, &q);
   MxPart sum = mx_no_part();
+  s_long[threadIdx.x] = mx_no_long_part();
   float high = -kMxInf;
   int4 own[Shared::OWN];
   u32 scales[SHAPE::SCALE_WORDS];
@@ -254,7 +282,10 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
       if (half == 0 && query < queries.n) highest[(u64)query * n_groups + row0 / group] = h;
       high = -kMxInf;
     }
+    if ((row0 - first) % kMxSumRows == kMxSumRows - kMxTile) mx_put_by(&sum, unit, &s_long[threadIdx.x]);
   }
+  mx_put_by(&sum, unit, &s_long[threadIdx.x]);
+  sum = {sum.m, (float)s_long[threadIdx.x].l, (float)s_long[threadIdx.x].e};
   sum = mx_join(sum, mx_shuffle_xor(sum, 32), unit);
   if (BIAS) mx_put_nan(nan, &sum);
   if (half == 0 && query < queries.n) parts[(u64)query * gridDim.x + part] = sum;

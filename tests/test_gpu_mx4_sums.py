@@ -5,6 +5,9 @@ p: an exponential (2 H), a factor for what float32 does not hold of the exponent
 The exponent itself is off by its rounding, H |s - lse| (with a bias twice, and its unit by H / 2 of it).  Three pieces of p are exact.  An instruction
 adds 16 rows of one piece and is off by 2 H of the sum at most, one after the other in a part of the rows: 6 H / 16 a row.  Up to three
 sums of waves are joined (3 H); parts are added in 64 bits, and so is what a long part has for every 4096 rows.  Together T = 8 H + 3 H |s - lse| + 6 H ceil(rows / 16).
+
+Log-sum-exp and entropy: exponentials are off by 3 H |s - m| + 2 H; a lane adds up its 16 rows of a tile (9 additions), 128 tiles
+one after the other (the rest in 64 bits), and some 40 sums of lanes, waves and parts follow: R = 180 H + 3 H |s - m|, and the roundings of lse's own size.
 """
 import math
 
@@ -162,3 +165,31 @@ def test_very_many_given_rows():
     for h in (None, torch.zeros(m, device="cuda")):
         d = hps.mx4_logprobs_backward(q, r, dev(given), dev(u), out.lse, out.entropy, h, scale=0.1).cpu().numpy()
         assert np.all(np.abs(d - want) <= off), np.max(np.abs(d - want) / off)
+
+
+@pytest.mark.parametrize("m,n,dim", [(32800, (1 << 24) + 77, 8), (16500, (1 << 24) + 33, 260)])
+@pytest.mark.parametrize("biased", [False, True])
+def test_log_probabilities_of_very_many_rows(m, n, dim, biased):
+    """Eight parts of two million rows: one term's worth of sums after the other that never is a whole number of anything."""
+    rows = hps.Mx4Rows.empty(n, dim, "cuda")
+    rows.codes.zero_()
+    rows.scales.fill_(127)
+    queries = hps.Mx4Rows.empty(m, dim, "cuda")
+    queries.codes.fill_(0x22)
+    queries.scales.fill_(127)
+    scale = 0.28
+    # (8 parts, 12 bytes a query each)
+    assert hps.lib().hps_mx4_logprobs_bytes(m, n, dim, 0) <= 8 * 12 * m + 256
+    for every in (64, 1000):
+        # the first two values of a row are a half, of every so many rows 1
+        rows.codes[:, 0] = 0x11
+        rows.codes[::every, 0] = 0x22
+        out = hps.mx4_logprobs(queries, rows, None, 0, scale, torch.zeros(n, device="cuda") if biased else None)
+        assert (out.lse == out.lse[0]).all() and (out.entropy == out.entropy[0]).all()
+        low = float(np.float32(scale))
+        high, k = 2 * low, -(-n // every)
+        l = k * math.exp(high) + (n - k) * math.exp(low)
+        lse, entropy = math.log(l), math.log(l) - (k * math.exp(high) * high + (n - k) * math.exp(low) * low) / l
+        r = H * (180 + 3 * low)
+        assert abs(float(out.lse[0]) - lse) <= r + 4 * H * lse
+        assert abs(float(out.entropy[0]) - entropy) <= 2 * r * (1 + low) + 8 * H * entropy
