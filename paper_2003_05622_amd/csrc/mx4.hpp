@@ -90,9 +90,6 @@ __device__ __forceinline__ MxEight mx_decode(u32 codes, u32 scale) {
 
 constexpr int kMxThreads = 256;
 
-// Lane groups a block's codes take: a group's lanes hold eight values each.
-__host__ __device__ constexpr int mx_group_lanes(u32 dim) { return dim <= 8 ? 1 : dim <= 16 ? 2 : 4; }
-
 template <bool BF16>
 __device__ __forceinline__ float4 load_values4(const void* base, u64 at) {
   if (BF16) {
@@ -288,20 +285,15 @@ __device__ __forceinline__ void mx_load_scales(const MxHeld& m, u32 row, u32 blo
     return;
   }
   // Eight scale bytes at a time, those of four steps of both halves; where fewer are left in the array, the last
-  // eight of it, shifted.
+  // eight of it, shifted.  (A row of such a shape has nine or more.)
   const u64 all = (u64)m.n * blocks;
 #pragma unroll
   for (int w = 0; w < SHAPE::SCALE_WORDS; ++w) {
     if (8 * w >= (int)blocks) { to[w] = 0; continue; }
+    const u64 at = first + 8 * w, from = min(at, all - 8);
     u64 eight;
-    if (all >= 8) {
-      const u64 at = first + 8 * w, from = min(at, all - 8);
-      __builtin_memcpy(&eight, m.scales + from, 8);
-      eight >>= 8 * (at - from);
-    } else {
-      eight = 0;
-      for (u32 i = 0; i < min(8u, blocks - 8 * w); ++i) eight |= (u64)m.scales[first + 8 * w + i] << (8 * i);
-    }
+    __builtin_memcpy(&eight, m.scales + from, 8);
+    eight >>= 8 * (at - from);
     to[w] = __builtin_amdgcn_perm((u32)(eight >> 32), (u32)eight, half ? 0x07050301u : 0x06040200u);
   }
   mx_clear_last_scale<SHAPE>(blocks, to);
@@ -454,22 +446,6 @@ template <typename SHAPE>
 __device__ __forceinline__ MxTile mx_products_shared(const int4* tile, const u32* scales, const MxRow<SHAPE>& b, u32 blocks) {
   MxTile d = mx_zero_tile();
   mx_steps_shared<SHAPE>(tile, scales, b, blocks, &d);
-  return d;
-}
-
-// The same step by step, for rows that a wave meets once: nothing is held between the steps.
-template <int WIDTH>
-__device__ __forceinline__ MxTile mx_products_once(const MxHeld& a, u32 a_row, const MxHeld& b, u32 b_row, u32 blocks) {
-  const u32 half = lane_id() / 32;
-  MxTile d = mx_zero_tile();
-#pragma unroll 4
-  for (u32 s = 0; s < blocks; s += 2) {
-    const u32 block = min(s + half, blocks - 1);
-    const int4 ca = mx_load_block<WIDTH>(a.codes + ((u64)a_row * blocks + block) * WIDTH);
-    int4 cb = mx_load_block<WIDTH>(b.codes + ((u64)b_row * blocks + block) * WIDTH);
-    if (s + half >= blocks) cb = make_int4(0, 0, 0, 0);
-    d = mx_step<0>(ca, a.scales[(u64)a_row * blocks + block], cb, b.scales[(u64)b_row * blocks + block], d);
-  }
   return d;
 }
 

@@ -5,7 +5,6 @@ namespace {
 
 constexpr uint64_t kMxMaxQueries = 1ull << 20;
 constexpr uint64_t kMxMaxRows = (1ull << 31) - 1;
-constexpr uint64_t kMxMaxBlocks = (1ull << 24) - 1;   // workgroups of 256 a launch may have
 constexpr uint64_t kMxMaxScores = 1ull << 40;      // scores of a call, more than a GPU has room for
 constexpr uint64_t kMxScoreGroups = 2048;          // workgroups of mx_scores that fill the GPU
 
@@ -139,19 +138,19 @@ hps_status hps_mx4_get(hps_table* t, const uint64_t* d_keys, uint64_t n, uint8_t
 hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
                           const float* d_bias, void* d_out, hps_value_type type, uint64_t stride, void* stream) {
   if (!mx_dim_ok(dim) || !mx_rows_ok(queries, dim, kMxMaxQueries) || !mx_rows_ok(rows, dim, kMxMaxRows) || !mx_scale_ok(scale) ||
-      (type != HPS_VALUES_F32 && type != HPS_VALUES_BF16) || stride < rows->n || stride > (1ull << 40))
+      (type != HPS_VALUES_F32 && type != HPS_VALUES_BF16) || stride < rows->n || stride > (1ull << 40) ||
+      rows->n * queries->n > kMxMaxScores)
     return HPS_EINVAL;
   if (queries->n == 0 || rows->n == 0) return HPS_OK;
   const bool bf16 = type == HPS_VALUES_BF16;
   if (!d_out || !mx_aligned(d_out, bf16 ? 2 : 4) || !mx_aligned(d_bias, 4)) return HPS_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hps_status rc = HPS_OK;
   mx_by_shape(dim, [&](auto shape) {
     typedef decltype(shape) Shape;
     const uint64_t row_groups = mx_ceil(rows->n, mx_score_tiles<Shape>() * kMxTile * (kMxThreads / kWave)), tiles = mx_ceil(queries->n, kMxTile);
     // a part of the queries for every workgroup, as long as that leaves enough of them
     const uint64_t part_tiles = mx_ceil(tiles, std::max<uint64_t>(1, kMxScoreGroups / row_groups)), parts = mx_ceil(tiles, part_tiles);
-    if (row_groups * parts > kMxMaxBlocks || rows->n * queries->n > kMxMaxScores) { rc = HPS_EINVAL; return; }
+    // (at most 2^23 workgroups)
     mx_by_flag(d_bias != nullptr, [&](auto biased) {
       mx_by_flag(bf16, [&](auto narrow) {
         // (1024 x 262 144, float32: 203 us past the L2, 300 through it; 333 x 100 003: 49 us past it, 27 through it)
@@ -164,7 +163,6 @@ hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows,
       });
     });
   });
-  if (rc != HPS_OK) return rc;
   return launch_ok() ? HPS_OK : HPS_EDEVICE;
 }
 
