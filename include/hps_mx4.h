@@ -32,6 +32,7 @@
 extern "C" {
 #endif
 
+/* What `type` says below (an int32_t there, as others than these two may be passed, and are refused). */
 typedef enum { HPS_VALUES_F32 = 0, HPS_VALUES_BF16 = 1 } hps_value_type;
 
 typedef struct {
@@ -52,7 +53,7 @@ size_t hps_mx4_row_scales(uint32_t dim);
  * 2^-127); values are rounded to the nearest code, ties to the even one, and what lies above 6
  * scales becomes 6.  A block with an infinite value or a NaN gets the scale byte 255.
  * Errors: HPS_EINVAL. */
-hps_status hps_mx4_quantize(const void* d_values, hps_value_type type, uint64_t n, uint32_t dim, uint64_t stride,
+hps_status hps_mx4_quantize(const void* d_values, int32_t type, uint64_t n, uint32_t dim, uint64_t stride,
                             uint8_t* d_codes, uint8_t* d_scales, float* d_rounded, void* stream);
 
 /* The values that n rows stand for: d_out [n, dim] float32, 16-byte aligned.  Errors: HPS_EINVAL. */
@@ -77,7 +78,7 @@ hps_status hps_mx4_get(hps_table* t, const uint64_t* d_keys, uint64_t n, uint8_t
  * (4-byte aligned) or bfloat16 (2-byte aligned, each score rounded to the nearest) by `type`.
  * Errors: HPS_EINVAL. */
 hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
-                          const float* d_bias, void* d_out, hps_value_type type, uint64_t stride, void* stream);
+                          const float* d_bias, void* d_out, int32_t type, uint64_t stride, void* stream);
 
 /* Over the scores of each query, none of which is stored:
  *   d_lse     [queries] float32: log of the sum of exp(score)

@@ -88,7 +88,7 @@ extern "C" {
 size_t hps_mx4_row_bytes(uint32_t dim) { return mx_dim_ok(dim) ? mx_row_bytes(dim) : 0; }
 size_t hps_mx4_row_scales(uint32_t dim) { return mx_dim_ok(dim) ? mx_blocks(dim) : 0; }
 
-hps_status hps_mx4_quantize(const void* d_values, hps_value_type type, uint64_t n, uint32_t dim, uint64_t stride,
+hps_status hps_mx4_quantize(const void* d_values, int32_t type, uint64_t n, uint32_t dim, uint64_t stride,
                             uint8_t* d_codes, uint8_t* d_scales, float* d_rounded, void* stream) {
   if (!mx_dim_ok(dim) || (type != HPS_VALUES_F32 && type != HPS_VALUES_BF16) || stride < dim || stride % 4) return HPS_EINVAL;
   if (n > (1ull << 40) || stride > (1ull << 40) / std::max<uint64_t>(n, 1)) return HPS_EINVAL;
@@ -136,7 +136,7 @@ hps_status hps_mx4_get(hps_table* t, const uint64_t* d_keys, uint64_t n, uint8_t
 }
 
 hps_status hps_mx4_scores(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
-                          const float* d_bias, void* d_out, hps_value_type type, uint64_t stride, void* stream) {
+                          const float* d_bias, void* d_out, int32_t type, uint64_t stride, void* stream) {
   if (!mx_dim_ok(dim) || !mx_rows_ok(queries, dim, kMxMaxQueries) || !mx_rows_ok(rows, dim, kMxMaxRows) || !mx_scale_ok(scale) ||
       (type != HPS_VALUES_F32 && type != HPS_VALUES_BF16) || stride < rows->n || stride > (1ull << 40) ||
       rows->n * queries->n > kMxMaxScores)

@@ -7,6 +7,8 @@
   image ships no clang sanitizer runtime, so undefined behaviour ends the process instead of
   being reported, and there is no AddressSanitizer for it) and the C ABI's argument checks
   (tests/test_abi.py: calls that return before anything touches a GPU) run against that build.
+* The same for the operators on frozen rows (tests/test_mx4.py: their argument checks, and the arithmetic of sizes behind
+  them), from the host side alone, beside the device code of an empty kernel.
 * The clamping of bags' offsets (csrc/pool.hpp), compiled for the host the same way, is given offsets of every kind.
 """
 import os
@@ -104,3 +106,27 @@ def test_bag_ranges_stay_inside_whatever_the_offsets(tmp_path):
     assert res.returncode == 0, res.stdout[-4000:]
     res = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=60)
     assert res.returncode == 0 and "bags ok" in res.stdout, (res.returncode, res.stdout[-4000:])
+
+
+def test_argument_checks_of_the_operators_on_frozen_rows_with_undefined_behaviour_traps(tmp_path):
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not os.path.exists(hipcc):
+        pytest.skip("no hipcc here")
+    (tmp_path / "empty.hip").write_text("#include <hip/hip_runtime.h>\n__global__ void nothing() {}\n")
+    host, empty, code, lib = (str(tmp_path / name) for name in ("host.o", "empty.hsaco", "code.o", "libhps_host.so"))
+
+    def run(*cmd):
+        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert res.returncode == 0, res.stdout[-4000:]
+        return res.stdout
+    run(hipcc, "--offload-arch=gfx950", "--cuda-host-only", "-O1", "-std=c++17", "-c", "-fPIC", "-w", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host",
+        "-fsanitize-trap=undefined", "-o", host, os.path.join(ROOT, "paper_2003_05622_amd", "csrc", "hps.hip"))
+    run(hipcc, "--offload-arch=gfx950", "--genco", "-O1", "-w", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-o", empty,
+        str(tmp_path / "empty.hip"))
+    name = [line.split()[-1] for line in run("nm", "-u", host).splitlines() if "__hip_fatbin" in line][0]
+    (tmp_path / "code.s").write_text('.section .hip_fatbin,"a"\n.p2align 12\n.globl %s\n%s:\n.incbin "%s"\n.section .note.GNU-stack,"",@progbits\n'
+                                     % (name, name, empty))
+    run("gcc", "-c", "-o", code, str(tmp_path / "code.s"))
+    run(hipcc, "-shared", "-o", lib, host, code)
+    rc, out = _run_pytest("test_mx4.py", {"HPS_LIB": lib})
+    assert rc == 0, out[-4000:]
