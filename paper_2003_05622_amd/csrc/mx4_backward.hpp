@@ -14,7 +14,7 @@
 // three are used where p is above 2^-6, which a query has at most 64 rows for.  The others' errors, independent of each other as long
 // as the probabilities differ, come to 2^-18.7 sqrt(sum p^2) <= 2^-21.7 of a row, as float32 itself leaves (lse is a float32 number:
 // a p is off by 2^-24 |lse| of itself).  Equal probabilities have equal errors, which add up (a query of zeros has nothing else):
-// all three are used too where rows of a tile have the same p.  That test takes 1.5 % of the time.  What no test sees (probabilities of a few sizes that
+// all three are used too where rows of a tile have the same p.  That test takes 1 % of the time.  What no test sees (probabilities of a few sizes that
 // take turns) stays below 2^-17 sum p |row|.
 // Without a gradient of the entropy c is p up to a factor per query, which the end applies.
 // mx_gradient_end adds the parts of the rows and the given rows.
@@ -169,6 +169,10 @@ struct MxOnes {
   __device__ __forceinline__ MxOnes() { asm("" : "+v"(minus_low), "+v"(minus_high)); }
 };
 
+__device__ __forceinline__ bool mx_same_pair(float a0, float a1, float b0, float b1) {
+  return ((u64)__float_as_uint(a1) << 32 | __float_as_uint(a0)) == ((u64)__float_as_uint(b1) << 32 | __float_as_uint(b0));
+}
+
 // Adds c row of 32 rows to the sums of 32 queries.  d: their products; values: the rows' unpacked columns.
 template <bool BIAS, bool ENTROPY, int BLOCKS>
 __device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float scale, const MxGradQuery<BIAS>& query, float unit,
@@ -183,8 +187,8 @@ __device__ __forceinline__ void mx_add_tile(MxTile d, const float* x_bias, float
     // (log p of a row far below, or out, is not multiplied with: its p is 0)
     d[i] = ENTROPY ? p[i] * __fmaf_rn(query.b, BIAS ? fmaxf(log2_p, -200.f) : log2_p, query.a) : p[i];
   }
-  // (two pairs: one alone is equal by chance in some tiles of a hundred)
-  const bool alike = p[0] == p[4] && p[1] == p[5] && p[0] > 0.f;
+  // Rows of the same p (not of rows that are out): two pairs, as one alone is equal by chance in some tiles of a hundred.
+  const bool alike = mx_same_pair(p[0], p[1], p[4], p[5]) && (!BIAS || p[0] > 0.f);
   const bool all_pieces = __any(most > kMxLarge || alike);
 #pragma unroll
   for (int step = 0; step < 2; ++step) {

@@ -55,6 +55,24 @@ def test_equal_probabilities_add_up(m, dim, biased):
         assert np.all(np.abs(d - want) <= t * np.abs(v) + 2 * H * np.abs(want)), (n, np.abs(d - want).max() / H)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -60, 1e-20, -1e-12])
+def test_equal_probabilities_of_different_products(scale):
+    """A scale next to nothing: the rows differ, their probabilities do not.  (The gradient has the scale as a factor, which is divided out.)"""
+    for n in list(range(66, 400, 13)) + [1025]:
+        rng = np.random.default_rng(n)
+        (q, _), (r, rv) = make(rng, 2, 64), make(rng, n, 64, 0.1, 0.0)
+        rv = np.abs(rv)
+        r.codes.bitwise_and_(0x77)    # (no signs: the mean of the rows is as large as they are)
+        lse = np.float32(math.log(n))
+        d = hps.mx4_logprobs_backward(q, r, torch.zeros((2, 1), dtype=torch.int32, device="cuda"), torch.ones((2, 1), device="cuda"),
+                                      torch.full((2,), float(lse), device="cuda"), scale=scale).cpu().numpy().astype(np.float64)
+        held = float(np.float32(scale))
+        p = math.exp(-float(lse))
+        want = rv[0] - p * rv.sum(axis=0)
+        t = H * (8 + 3 * math.log(n) + 6 * math.ceil(rows_of_a_part(2, n, 64) / 16))
+        assert np.all(np.abs(d / held - want) <= t * p * rv.sum(axis=0) + 3 * H * np.abs(want)), n
+
+
 @pytest.mark.parametrize("n", [2, 3, 7, 13, 24, 32, 47])
 @pytest.mark.parametrize("dim", [8, 64, 260])
 def test_few_rows_with_large_probabilities(n, dim):
