@@ -282,8 +282,8 @@ mx_gradient(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_bytes, flo
             u32 n_given, const float* __restrict__ d_entropy, u32 query_groups, MxPartRows part, void* __restrict__ parts) {
   constexpr int BLOCKS = COLUMNS / 32;
   constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;           // of 8 bytes, a tile's unpacked values
-  __shared__ uint2 s_rows[2][kMxStageTiles][kTileWords];
-  __shared__ float s_bias[kMxGradWaves][kMxTile];
+  __shared__ __align__(16) uint2 s_rows[2][kMxStageTiles][kTileWords];
+  __shared__ __align__(16) float s_bias[kMxGradWaves][kMxTile];
   const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const u32 splits = kMxGradWaves / query_groups, split = wave / query_groups;
   const u32 query0 = (blockIdx.y * query_groups + wave % query_groups) * (QT * kMxTile) + lane % 32;
@@ -390,8 +390,8 @@ mx_gradient_shared(MxHeld queries, MxHeld rows, u32 dim, u32 blocks, u32 row_byt
   constexpr u32 kTileWords = BLOCKS * 2 * kWave * 2;
   typedef MxShared<SHAPE> Shared;
   __shared__ int4 s_tile[2][Shared::UNITS];
-  __shared__ uint2 s_rows[2][kStage][kTileWords];
-  __shared__ float s_bias[2][kMxTile];
+  __shared__ __align__(16) uint2 s_rows[2][kStage][kTileWords];
+  __shared__ __align__(16) float s_bias[2][kMxTile];
   const u32 lane = lane_id(), half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const u32 mine = (blockIdx.y * (kMxThreads / kWave) + wave) * kMxTile + lane % 32;
   const u32 first = part.first(), end = part.end(rows.n), col0 = blockIdx.z * COLUMNS;

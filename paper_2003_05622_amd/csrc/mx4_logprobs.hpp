@@ -127,7 +127,7 @@ template <typename SHAPE, bool BIAS, int QT>
 __global__ void __launch_bounds__(kWave) HPS_MX_WAVES
 mx_softmax(MxHeld queries, MxHeld rows, u32 blocks, float scale, const float* __restrict__ bias, u32 part_rows, u32 group,
            u32 n_groups, MxPart* __restrict__ parts, float* __restrict__ highest) {
-  __shared__ float s_bias[kMxTile];
+  __shared__ __align__(16) float s_bias[kMxTile];
   __shared__ MxLongPart s_long[QT][kWave];
   const u32 lane = lane_id(), half = lane / 32, part = blockIdx.x;
   const u32 query0 = blockIdx.y * (QT * kMxTile) + lane % 32;
@@ -222,7 +222,7 @@ mx_softmax_shared(MxHeld queries, MxHeld rows, u32 blocks, float scale, const fl
                   u32 n_groups, MxPart* __restrict__ parts, float* __restrict__ highest) {
   typedef MxShared<SHAPE> Shared;
   __shared__ int4 s_tile[2][Shared::UNITS];
-  __shared__ float s_bias[2][kMxTile];
+  __shared__ __align__(16) float s_bias[2][kMxTile];
   __shared__ MxLongPart s_long[kMxThreads];
   const u32 lane = lane_id(), half = lane / 32, part = blockIdx.x;
   const u32 query = (blockIdx.y * (kMxThreads / kWave) + threadIdx.x / kWave) * kMxTile + lane % 32;
