@@ -23,13 +23,16 @@ uint64_t mx_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 // How the rows are dealt out over the waves: so many parts that the GPU is full, a multiple of 8, so that all waves of
 // a part share an XCD and with it the L2 that holds its rows.
 constexpr uint64_t kMxWaves = 4096;
+// Up to so many queries the end of the log probabilities takes 16 waves a query, beyond four: 64 x 262 144, 64 wide, best 8: 21 us (25 with four), 256: 33
+// (35), 320: 42 (46 with 16), 1024: 75 (95).
 constexpr uint64_t kMxFewQueries = 256;
 // Workgroups of mx_gradient: as many as run at once (two on a CU, four of the narrow ones with one query tile a wave), so that all end together.
 constexpr uint64_t kMxGradGroups = 512;
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
 };
-// Query tiles a wave of mx_softmax holds: two share what is read of the rows, unless that leaves much of the last ones empty.
+// Query tiles a wave of mx_softmax holds: two share what is read of the rows, unless that leaves much of the last ones empty.  (1024 x 262 144, 64 wide:
+// 59 us, 62 with one; 160 x 524 288, five tiles: 28, 31 with two; 64 x 524 288: 16.5, 15.1 with one.)
 int mx_wave_tiles(uint64_t n_queries, uint32_t dim) {
   const uint64_t tiles = mx_ceil(n_queries, kMxTile);
   return mx_blocks(dim) <= 8 && (tiles % 2 == 0 || tiles > 8) ? 2 : 1;
@@ -48,7 +51,8 @@ MxSplit mx_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top
   s.groups = top ? mx_ceil(n_rows, s.group) : 0;
   return s;
 }
-// Whether the waves of a workgroup share the rows' tiles: rows of more than 256 values, and queries for at least three of its four waves.
+// Whether the waves of a workgroup share the rows' tiles: rows of more than 256 values, and queries for at least three of its four waves.  (Log
+// probabilities, 65 536 rows of 1024: 1024 queries 86 us, 169 without sharing, 96 28 and 35, 64 27 and 28; of 512: 1024 43 and 78, 32 12.8 and 12.5.)
 bool mx_shares_rows(uint64_t n_queries, uint32_t dim) { return mx_blocks(dim) > 8 && n_queries > 2 * kMxTile; }
 MxSplit mx_softmax_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim, uint32_t top) {
   if (mx_shares_rows(n_queries, dim)) return mx_split(n_queries, n_rows, dim, top, kMxThreads / kWave, kMxWaves / (kMxThreads / kWave));
@@ -246,6 +250,7 @@ static bool mx_gradient_shares(uint64_t n_queries, uint32_t dim) { return mx_blo
 static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t dim) {
   MxGradSplit s;
   const uint64_t tiles = mx_ceil(n_queries, kMxTile);
+  // (two where there are enough of them: 1024 x 524 288, 64 wide, 188 us, 196 with one; 192 x 262 144 41, 43 with two; 224 43.5, 40 with one)
   s.wave_tiles = dim <= 64 && tiles > 6 ? 2 : 1;
   const uint64_t waves = mx_ceil(tiles, s.wave_tiles);
   s.query_groups = waves > 2 || mx_gradient_shares(n_queries, dim) ? 4 : waves;
@@ -330,7 +335,7 @@ hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_
 #define HPS_MX_END(WAVES)                                                                                                    \
   mx_gradient_end<B, E, WAVES><<<blocks_end, WAVES * kWave, 0, s>>>(mx_held(rows), (u32)m, dim, blocks, row_bytes, scale, d_bias, \
                                                                     d_given, d_dlogp, n_given, d_workspace, (u32)p.parts, p.wide, d_dqueries)
-      // (few values: more waves each; many: as many workgroups at once as there are)
+      // (few values: more waves each, 1 x 1 M, 64 wide, 28.6 us, 31.6 with eight; many: as many workgroups at once as there are, 1024 x 524 288 188, 187 with 16)
       if (blocks_end <= 256) HPS_MX_END(16);
       else HPS_MX_END(8);
 #undef HPS_MX_END

@@ -397,7 +397,7 @@ __device__ __forceinline__ u64 mx_most(u64 c) {
 }
 
 // The best groups: every thread takes the best of the groups that fall to it.  `top` or more sets of threads have a best one each;
-// the worst of these is a bound that `top` groups reach, and some four times as many do at most (where top is above 16, a wave
+// the worst of these is a bound that `top` groups reach, and mostly few others (where top is above 16, a wave
 // sorts what its threads have and gives its ceil(top / WAVES)-th).  Those that do are collected and sorted.  The rows of the best groups go the
 // same way, with the last group's highest score as the bound.
 template <int WIDTH, bool BIAS, int WAVES>
