@@ -68,8 +68,8 @@ hps_status hps_mx4_get(hps_table* t, const uint64_t* d_keys, uint64_t n, uint8_t
 
 /* What a query and a row of the catalogue give:
  *   score = scale * <query, row> + bias[row],  rounded to float32 once (the product of the
- * held values is summed in float32).  scale: a host value, at most 2^100 in magnitude; scores should stay
- * below 2^126 (beyond, results may be NaN).
+ * held values is summed in float32).  scale: a host value, at most 2^100 in magnitude; scores, and the
+ * products before they are scaled, should stay below 2^126 (beyond, results may be NaN).
  *   d_bias [rows] float32 or NULL.  A bias that is not finite takes its row out: its score is
  *   -infinity, whatever its codes and the query's are.  The lowest finite value is a bias like any other.
  * At most 2^20 queries and fewer than 2^31 rows; either may be 0. */

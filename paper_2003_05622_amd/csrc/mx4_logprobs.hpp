@@ -34,9 +34,11 @@ struct MxPart {
 };
 constexpr float kMxLowest = -3.402823466e38f;
 __device__ __forceinline__ MxPart mx_no_part() { return {kMxLowest, 0.f, 0.f}; }
+// The power of two by which sums for m `from` count for a higher m.  (The difference may be beyond float32, and the unit 0.)
+__device__ __forceinline__ float mx_drop(float from, float m, float unit) { return fmaxf(from - m, kMxLowest) * unit; }
 // Brings a part to a higher m.
 __device__ __forceinline__ void mx_raise(MxPart* a, float m, float unit) {
-  const float by = (a->m - m) * unit, f = exp2f(by);
+  const float by = mx_drop(a->m, m, unit), f = exp2f(by);
   a->e = f == 0.f ? 0.f : (a->e + a->l * by) * f;       // (`by` may be too large to multiply with)
   a->l *= f;
   a->m = m;
@@ -64,7 +66,7 @@ struct MxLongPart {
 __device__ __forceinline__ MxLongPart mx_no_long_part() { return {0.0, 0.0, kMxLowest}; }
 // Adds a lane's sums (m of which is the highest so far) and begins new ones.
 __device__ __forceinline__ void mx_put_by(MxPart* a, float unit, MxLongPart* to) {
-  const float by = (to->m - a->m) * unit;
+  const float by = mx_drop(to->m, a->m, unit);
   const double f = exp2f(by), e = f == 0.0 ? 0.0 : (to->e + to->l * by) * f;
   *to = {to->l * f + a->l, e + a->e, a->m};
   a->l = a->e = 0.f;
@@ -92,7 +94,7 @@ __device__ __forceinline__ void mx_add_rows(const MxTile& d, float scale, const 
   *high = fmaxf(*high, most[0]);
   // (seldom, once a wave has seen some rows)
   if (__any(most[0] > sum->m)) {
-    const float m = fmaxf(sum->m, most[0]), by = (sum->m - m) * unit, f = exp2_fast(by);
+    const float m = fmaxf(sum->m, most[0]), by = mx_drop(sum->m, m, unit), f = exp2_fast(by);
     sum->e = f == 0.f ? 0.f : (sum->e + sum->l * by) * f;
     sum->l *= f;
     sum->m = m;

@@ -113,3 +113,26 @@ def test_a_pooled_row_that_is_not_finite_goes_through():
     d = hps.mx4_logprobs_backward(queries, rows, None, None, got.lse, got.entropy, torch.ones(4, device="cuda"), 1.0, bias)
     assert (d == 0).all() and (hps.mx4_scores(queries, rows, 1.0, bias) == -INF).all()
     assert np.isneginf(ref.scores(np.full((1, 64), np.nan), np.zeros((50, 64)), 1.0, bias.cpu().numpy())).all()
+
+
+@pytest.mark.parametrize("dim,m", [(8, 3), (64, 40), (300, 70)])
+def test_a_scale_of_nothing_and_large_products(dim, m):
+    """All scores are 0, however large the products are that are scaled."""
+    n = 5000
+    rng = np.random.default_rng(dim)
+    queries, rows = hps.Mx4Rows.empty(m, dim, "cuda"), hps.Mx4Rows.empty(n, dim, "cuda")
+    for held in (queries, rows):
+        held.codes.zero_()
+        held.codes[:, 0] = dev(rng.integers(0, 256, size=held.n, dtype=np.uint8))
+        held.scales.fill_(127)
+        held.scales[:, 0] = 127 + 57                # products up to 72 x 2^114
+    given = torch.full((m, 1), 4321, dtype=torch.int32, device="cuda")
+    got = hps.mx4_logprobs(queries, rows, given, 4, 0.0)
+    log_n = float(np.log(n))
+    # (as many equal terms: sums of whole numbers, one logarithm)
+    assert (got.lse - log_n).abs().max() <= 8 * 2.0 ** -24 * log_n and (got.entropy - log_n).abs().max() <= 8 * 2.0 ** -24 * log_n
+    assert (got.logp + log_n).abs().max() <= 8 * 2.0 ** -24 * log_n
+    assert (got.top_index == torch.arange(4, dtype=torch.int32, device="cuda")).all()
+    assert (hps.mx4_scores(queries, rows, 0.0) == 0).all()
+    d = hps.mx4_logprobs_backward(queries, rows, given, torch.ones((m, 1), device="cuda"), got.lse, got.entropy, torch.ones(m, device="cuda"), 0.0)
+    assert (d == 0).all()
