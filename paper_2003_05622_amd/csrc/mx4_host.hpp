@@ -28,6 +28,7 @@ constexpr uint64_t kMxWaves = 4096;
 constexpr uint64_t kMxFewQueries = 256;
 // Workgroups of mx_gradient: as many as run at once (two on a CU, four of the narrow ones with one query tile a wave), so that all end together.
 constexpr uint64_t kMxGradGroups = 512;
+constexpr uint64_t kMxPartsBytes = 128ull << 20;
 struct MxSplit {
   uint64_t query_tiles, part_rows, parts, group, groups;
 };
@@ -261,6 +262,9 @@ static MxGradSplit mx_grad_split(uint64_t n_queries, uint64_t n_rows, uint32_t d
   s.part_rows = mx_ceil(mx_ceil(n_rows, wanted), kMxStageRows) * kMxStageRows;
   // (waves that share the rows join their sums at the end of the part: each has so many rows at most)
   if (s.query_groups < kMxGradWaves) s.part_rows = std::min<uint64_t>(s.part_rows, kMxSumRows * (kMxGradWaves / s.query_groups));
+  // More parts than run at once rather than long ones, as long as their sums lie in the last-level cache.  (1024 x 131 072, 512 / 1024 wide: 516 / 1451 us,
+  // 533 / 1494 with long parts.)
+  else if (mx_ceil(n_rows, kMxSumRows) * n_queries * dim * sizeof(float) <= kMxPartsBytes) s.part_rows = std::min<uint64_t>(s.part_rows, kMxSumRows);
   s.parts = mx_ceil(n_rows, s.part_rows);
   s.wide = s.query_groups == kMxGradWaves && s.part_rows > kMxSumRows;
   return s;

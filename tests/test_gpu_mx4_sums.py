@@ -109,7 +109,7 @@ def test_two_probabilities_add_up():
 
 
 # (queries, rows, dim): so many queries that one part holds all of the rows, or nearly; waves that hold two query tiles and one, and waves that share the rows
-LONG = [(131072, 300007, 16), (131077, 70001, 64), (65540, 40001, 128), (32768, 20011, 300), (8200, 8193, 1024), (8200, 12288, 1000)]
+LONG = [(131072, 300007, 16), (131077, 70001, 64), (65540, 40001, 128), (32768, 20011, 300), (8200, 16385, 1024), (8200, 20480, 1000)]
 
 
 @pytest.mark.parametrize("m,n,dim", LONG)
@@ -131,7 +131,7 @@ def test_very_many_rows_in_one_part(m, n, dim, biased):
     assert np.all(np.abs(d - want) <= t * np.abs(v) + 2 * H * np.abs(want)), np.abs(d - want).max() / H
 
 
-@pytest.mark.parametrize("m,n,dim", [(65600, 20011, 64), (8300, 8300, 260), (65536, 4097, 16)])
+@pytest.mark.parametrize("m,n,dim", [(65600, 40011, 64), (33000, 20011, 260), (65536, 4097, 16)])
 @pytest.mark.parametrize("kind", ["plain", "entropy", "biased"])
 def test_long_parts_give_what_short_ones_give(m, n, dim, kind):
     """Some of many queries against the same ones alone, whose parts are short."""
