@@ -8,8 +8,8 @@
  *              outputs and workspaces are different buffers.  No output may overlap an
  *              input.  All of them may be captured into a HIP graph and replayed.
  *
- * What it is for: a trainer's rows (a catalogue of items or ads) are frozen for serving, an
- * eighth of their float32 size; pooled rows become queries; a request asks for the best rows of
+ * What it is for: a trainer's rows (a catalogue of items or ads) are frozen for serving, in 17 bytes
+ * for 32 values; pooled rows become queries; a request asks for the best rows of
  * the catalogue, a trainer for the log probability of the rows that were chosen, and for the
  * gradient that goes on into hps_push.  (A teacher's best rows as the given ones and minus its
  * probabilities as d_dlogp: distillation from the teacher's top scores.)

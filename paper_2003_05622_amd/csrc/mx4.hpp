@@ -177,7 +177,7 @@ mx_dequantize(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ sca
 }
 
 // Rows of the table by key.  As get_rows: a wave finds 64 keys, one per lane, and then goes through their
-// blocks, a lane group per block.  2 M keys of 8 M, dim 32: 87 us (get_rows 162, and 48 to quantise what it gives).
+// blocks, a lane group per block.  2 M keys of 8 M, dim 32: 92 us (get_rows 167, and 52 to quantise what it gives).
 template <bool BF16, int GL>
 __global__ void __launch_bounds__(kRowThreads)
 mx_get(TableView t, const u64* __restrict__ keys, u64 n_keys, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,

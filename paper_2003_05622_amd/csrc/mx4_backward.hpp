@@ -19,9 +19,9 @@
 // Without a gradient of the entropy c is p up to a factor per query, which the end applies.
 // mx_gradient_end adds the parts of the rows and the given rows.
 //
-// What bounds it: vector and matrix instructions, of which the GPU does hardly more than one kind at a time: 72 vector instructions (16
-// of them exponentials) and 9 of the matrix unit for 32 x 32 scores at 64 values a row, 164 us one after the other for 1024
-// queries and 0.5 M rows, 177 measured and 8 for the end.
+// What bounds it: vector and matrix instructions, of which the GPU does hardly more than one kind at a time: 74 vector instructions (16
+// of them exponentials) and 9 of the matrix unit for 32 x 32 scores at 64 values a row, 166 us one after the other for 1024
+// queries and 0.5 M rows, 181 measured and 8 for the end.
 #pragma once
 
 #include "mx4_logprobs.hpp"

@@ -12,8 +12,8 @@
 // that was not chosen (its highest score is higher, or equal and its row number lower).
 //
 // What bounds them.  mx_softmax: the vector unit; 64 scores take one exponential (8 cycles) and, of 4 cycles each, half a
-// maximum, two multiply-adds and an addition: 180 us for 1024 queries and 1 M rows at the 2.0 GHz the GPU keeps then, 212 measured
-// (94 % busy), of which the matrix unit needs 7 % at 64 values a row.  With one query, reading: 142 MB in 33 us.  So a
+// maximum, two multiply-adds and an addition: 180 us for 1024 queries and 1 M rows at the 2.0 GHz the GPU keeps then, 215 measured
+// (93 % busy), of which the matrix unit needs 7 % at 64 values a row.  With one query, reading: 142 MB in 33 us.  So a
 // maximum is taken of products, not scores, the scale goes into the exponent's factor, and sums are only raised to a new
 // maximum when a wave has one.  mx_finish: some eight steps that each wait for the one before, 14 us for one query, 22 for 1024.
 #pragma once

@@ -5,7 +5,7 @@
 // neighbouring rows of a query (tile t holds rows RT j + t): a store writes RT neighbouring scores a lane, whole lines a wave.
 // A wave holds RT x 32 rows and goes through the query tiles of its part; the rows' operands stay in
 // registers, the queries' come out of the caches, those of wide rows out of LDS, where the waves of a workgroup share them.
-// 1024 x 262 144 float32 scores (1.07 GB): 203 us at 16 to 256 values a row (5.3 TB/s), 212 at 512, 290 at 1024, where the operands'
+// 1024 x 262 144 float32 scores (1.07 GB): 204 us at 16 values a row (5.3 TB/s), 210 at 256, 214 at 512, 287 at 1024, where the operands'
 // way to the matrix unit takes over (1.9 PFLOP/s).
 #pragma once
 

@@ -8,7 +8,8 @@ queries of the same form, log probabilities over the scores, and the gradient of
     table.push(d)
 
 Tensors are torch CUDA tensors on one GPU; work goes to that GPU's current stream.  Argument marshalling only; nothing is
-kept between calls.
+kept between calls.  Results are no part of autograd's graph, whatever the arguments are: gradients are asked for by
+mx4_logprobs_backward, and go on into push() as above (quantising counts as the identity).
 """
 from __future__ import annotations
 
