@@ -112,7 +112,8 @@ hps_status hps_mx4_logprobs(const hps_mx4_rows* queries, const hps_mx4_rows* row
  *   d_dentropy        [queries] or NULL
  * A query that no row is left for has a gradient of 0, one that meets a NaN score of NaN.
  *   d_workspace       hps_mx4_logprobs_backward_bytes() bytes, 256-byte aligned
- * Two calls with the same inputs give the same bits.  Errors: HPS_EINVAL, HPS_ENOMEM. */
+ * Two calls with the same inputs give the same bits; those of a query may depend on which others share the call (by less than
+ * 2^-16 of the rows' magnitudes, weighted as they count).  Errors: HPS_EINVAL, HPS_ENOMEM. */
 size_t hps_mx4_logprobs_backward_bytes(uint64_t n_queries, uint64_t n_rows, uint32_t dim);
 hps_status hps_mx4_logprobs_backward(const hps_mx4_rows* queries, const hps_mx4_rows* rows, uint32_t dim, float scale,
                                      const float* d_bias, const float* d_lse, const float* d_entropy,

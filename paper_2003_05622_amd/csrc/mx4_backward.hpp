@@ -15,7 +15,7 @@
 // as the probabilities differ, come to 2^-18.7 sqrt(sum p^2) <= 2^-21.7 of a row, as float32 itself leaves (lse is a float32 number:
 // a p is off by 2^-24 |lse| of itself).  Equal probabilities have equal errors, which add up (a query of zeros has nothing else):
 // all three are used too where rows of a tile have the same p.  That test takes 1 % of the time.  What no test sees (probabilities of a few sizes that
-// take turns) stays below 2^-17 sum p |row|.
+// take turns) stays below 2^-17 sum |c| |row|.
 // Without a gradient of the entropy c is p up to a factor per query, which the end applies.
 // mx_gradient_end adds the parts of the rows and the given rows.
 //

@@ -211,3 +211,46 @@ def test_log_probabilities_of_very_many_rows(m, n, dim, biased):
         r = H * (180 + 3 * low)
         assert abs(float(out.lse[0]) - lse) <= r + 4 * H * lse
         assert abs(float(out.entropy[0]) - entropy) <= 2 * r * (1 + low) + 8 * H * entropy
+
+
+def test_long_parts_captured_and_on_two_streams():
+    """Several launches add up in one workspace: replays with new inputs, and two such calls at once, give what a call alone gives."""
+    m, n, dim = 66000, 70001, 32
+    gen = torch.Generator(device="cuda")
+
+    def inputs(seed):
+        gen.manual_seed(seed)
+        q = hps.mx4_quantize(torch.randn((m, dim), generator=gen, device="cuda"))
+        r = hps.mx4_quantize(torch.randn((n, dim), generator=gen, device="cuda"))
+        given = torch.randint(0, n, (m, 1), generator=gen, device="cuda", dtype=torch.int32)
+        return q, r, given, torch.randn((m, 1), generator=gen, device="cuda")
+
+    def both(q, r, given, u):
+        out = hps.mx4_logprobs(q, r, given, 0, 0.3)
+        return out.lse, hps.mx4_logprobs_backward(q, r, given, u, out.lse, out.entropy, scale=0.3)
+    assert hps.lib().hps_mx4_logprobs_backward_bytes(m, n, dim) <= 8 * m * dim + 256
+    held = inputs(0)
+    other = inputs(100)
+    want_other = both(*other)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        both(*held)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both(*held)
+    for turn in range(3):
+        for to, of in zip(held, inputs(turn + 1)):
+            if isinstance(to, hps.Mx4Rows):
+                to.codes.copy_(of.codes)
+                to.scales.copy_(of.scales)
+            else:
+                to.copy_(of)
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            at_once = both(*other)
+        torch.cuda.synchronize()
+        want = both(*held)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(at_once[0], want_other[0]) and torch.equal(at_once[1], want_other[1])
